@@ -457,6 +457,134 @@ int tl_hw_box_offsets(const tl_hw_desc* desc, const int32_t* d_coords, int64_t n
 int tl_hw_box_load(const tl_hw_desc* desc, const void* d_src_tilemajor, uint64_t src_bytes, const int32_t* d_coords,
                    int64_t n_boxes, void* d_dst, void* cuda_stream);
 
+/* ------------------------------------------------ key/value cache for drafted tokens */
+
+/*
+ * A step of a decoder that drafts tokens and checks them together: the products above give the step's queries, keys
+ * and values; tl_kv_append quantises keys and values into a paged cache; tl_tree_attention attends over it, every
+ * token seeing its request's context and its own branch of the draft tree; tl_tree_verify decides with the target's
+ * probabilities which drafts are kept; tl_kv_commit moves the kept tokens' cache rows together.  tl_kv_read gives
+ * rows back in bf16 or fp32.
+ *
+ * The cache is a pool of pages.  A page holds page_tokens tokens of every key/value head; within it the tokens of one
+ * head are one contiguous block, page_tokens rows of head_dim elements (packed strides: [page][head][token][dim]),
+ * the memory tile of this library applied to the cache: 32 tokens x 128 bytes are 4 KB.
+ *
+ * Formats.  TL_KV_BF16 holds the values rounded to bf16.  TL_KV_E4M3 and TL_KV_INT8 hold 8-bit codes and, per token
+ * and head, one fp32 scale: with a = max |x| over the head_dim elements, scale = a * c with c = 1/448 (E4M3) or 1/127
+ * (INT8) in fp32, code = x / scale (fp32) rounded to the nearest code, ties to even.  The value held is code * scale.  A row of zeros has scale 0; a row with an infinity or a NaN has scale NaN and reads back as NaN.
+ */
+typedef enum { TL_KV_BF16 = 0, TL_KV_E4M3 = 1, TL_KV_INT8 = 2 } tl_kv_format;
+typedef enum { TL_ELEM_BF16 = 0, TL_ELEM_F32 = 1 } tl_elem;
+
+typedef struct tl_kv_cache {
+    void* k;                    /* device, keys; 16-byte aligned */
+    void* v;                    /* device, values, same strides */
+    float* k_scale;             /* device, 16-byte aligned; NULL for TL_KV_BF16 */
+    float* v_scale;
+    int64_t pages;
+    int64_t page_stride, head_stride, token_stride;     /* elements, each a multiple of 16 bytes; all 0: packed */
+    int64_t scale_page_stride, scale_head_stride;       /* floats, multiples of 4; both 0: packed [page][head][token].
+                                                           The scales of a page's tokens are contiguous. */
+    int32_t format;             /* tl_kv_format */
+    int32_t heads, head_dim;    /* head_dim 64, 128 or 256 */
+    int32_t page_tokens;        /* power of two, 16 .. 1024 */
+} tl_kv_cache;
+
+/*
+ * One step's requests.  Request b owns the rows token_offsets[b] .. token_offsets[b + 1] - 1 of the step's arrays; its
+ * i-th row stands at position start[b] + i of its sequence, which lives in page page_table[b][position / page_tokens]
+ * of the pool.  All four arrays are read on the device, so a captured step follows their contents.  A position past
+ * the table or a page number outside [0, pages) is never touched: the row is not written / not attended to / reads
+ * back as zeros, and tl_device_status() reports it (TL_ERR_TIMEOUT, detail 0xA00).  Only the table's entries that
+ * hold a request's tokens are read.
+ */
+typedef struct tl_kv_batch {
+    const int32_t* page_table;      /* device [requests][table_stride] */
+    const int32_t* start;           /* device [requests] */
+    const int32_t* token_offsets;   /* device [requests + 1], non-decreasing, from 0 to tokens */
+    int64_t table_stride;           /* entries per request, >= 1 */
+    int32_t requests;
+    int32_t tokens;                 /* rows in total */
+} tl_kv_batch;
+
+/*
+ * Quantises the step's keys and values into the cache.  d_k, d_v: [tokens][heads][head_dim] of type elem, the row of
+ * a token row_stride elements after the last one, its heads contiguous (so both may be column ranges of one fused
+ * product's output); pointers and strides multiples of 16 bytes.  One kernel, asynchronous on cuda_stream.
+ */
+int tl_kv_append(const tl_kv_cache* cache, const tl_kv_batch* batch, const void* d_k, const void* d_v, int elem,
+                 int64_t row_stride, void* cuda_stream);
+/*
+ * Reads back, in the element type elem, the positions that tl_kv_append with the same batch writes (start = 0 and
+ * offsets over whole sequences give whole contexts).  Layout of d_k, d_v as above.  Asynchronous.
+ */
+int tl_kv_read(const tl_kv_cache* cache, const tl_kv_batch* batch, void* d_k, void* d_v, int elem, int64_t row_stride,
+               void* cuda_stream);
+/*
+ * Moves the cache rows of the tokens that were kept: the row of position start[b] + accepted[b][i] goes to position
+ * start[b] + i, for i < n_accepted[b].  accepted: device [requests][accepted_stride], increasing within a request
+ * (what tl_tree_verify writes).  new_start (may be NULL, may be batch->start itself): device [requests], receives
+ * start + n_accepted.  An index outside the request's rows, or below i, is skipped and reported (detail 0xB00).
+ * Codes and scales move as they are.  Asynchronous.
+ */
+int tl_kv_commit(const tl_kv_cache* cache, const tl_kv_batch* batch, const int32_t* d_accepted, int64_t accepted_stride,
+                 const int32_t* d_n_accepted, int32_t* d_new_start, void* cuda_stream);
+
+/*
+ * The visibility masks of draft trees: parents[row] is the parent's index within the request (-1 for the root, always
+ * below the row's own index); bit j of d_mask[row][j / 32] is set when token j is the row's token or an ancestor of
+ * it.  mask_words: words per row, at least 1; tokens past 32 * mask_words are left out.  Asynchronous.
+ */
+int tl_tree_mask(const int32_t* d_parents, const int32_t* d_token_offsets, int requests, int tokens, uint32_t* d_mask,
+                 int mask_words, void* cuda_stream);
+
+/*
+ * Attention of the step's tokens over the cache, which already holds their own keys and values:
+ *     out[i][h] = sum_j softmax_j(scale * q[i][h] . k[j][h / (q_heads / heads)]) v[j][...]
+ * over the positions j that row i sees: all of its request's context (j < start[b]), and of the step's own tokens
+ * those whose bit is set in d_mask[i] (d_mask NULL: tokens 0 .. i of the request, a causal chain; one token per
+ * request is ordinary decoding).  A token past the mask's words is not seen.  A row that sees nothing gives zeros
+ * and lse = -infinity.  What a masked position holds (infinity, NaN, never written) has no influence.
+ *   d_q, d_out  bf16 [tokens][q_heads][head_dim], rows q_stride / out_stride elements apart, heads contiguous;
+ *               pointers and strides multiples of 16 bytes.
+ *   q_heads     a multiple of cache->heads.
+ *   d_lse       NULL, or fp32 [tokens][q_heads]: natural logarithm of the sum of exp(scale * q . k).
+ * Scores, softmax statistics and sums are fp32.  Scratch for sequences that several CTAs share comes from the
+ * workspace (tl_tree_attention_workspace_bytes; tl_set_workspace or the internal one).  Asynchronous.
+ */
+int tl_tree_attention(const tl_kv_cache* cache, const tl_kv_batch* batch, const void* d_q, int64_t q_stride, int q_heads,
+                      const uint32_t* d_mask, int mask_words, float scale, void* d_out, int64_t out_stride, float* d_lse,
+                      void* cuda_stream);
+/* Workspace of such a call on the current device (0 for arguments the call would refuse). */
+size_t tl_tree_attention_workspace_bytes(const tl_kv_cache* cache, const tl_kv_batch* batch, int q_heads);
+
+/*
+ * Verification of draft trees (a chain is a tree of single children) against the target's distribution, with given
+ * random numbers.  Rows as in tl_kv_batch: request b owns rows token_offsets[b] .. token_offsets[b + 1] - 1, its row 0
+ * is the tree's root (the last token that is certain), parents as in tl_tree_mask.
+ *   d_target   fp32 [tokens][vocab], rows target_stride apart: the target's distribution after each row's token.
+ *   d_draft    fp32 [tokens][vocab], rows draft_stride apart: the distribution that the children of a row were drawn
+ *              from, independently; or NULL: the children were chosen without chance.
+ *   d_tokens   int32 [tokens]: drafted token ids (the root's is not read).
+ *   d_accept, d_sample  fp32 uniform numbers in [0, 1): one per row, one per request.
+ * From the root on: let r = p (the node's row of d_target), q its row of d_draft, S = 1.  Its children, in index order:
+ * child c with token x is kept when accept[c] * q(x) * S < r(x), and the walk goes on from it; else
+ * r = max(r - S q, 0), S = sum of r, and the next child is tried (if S is then 0: r = p, and no further child is
+ * tried).  Without d_draft q is 1 at x and 0 elsewhere, r(x) becomes 0 and S becomes S - min(r(x), S).  Where no child
+ * is kept the next token is drawn from r: the first id whose running sum of r exceeds sample[b] * (sum of r) (the last
+ * id with r > 0 at most; r = p if r is empty; -1 if p is too).  Kept tokens and the drawn one are then distributed as
+ * the target's own.  Probabilities that are negative or NaN, and ids outside [0, vocab), count as zero.  Sums over the
+ * vocabulary are fp64.
+ *   d_accepted    int32 [requests][accepted_stride]: rows kept, within the request, root first, then -1.
+ *   d_n_accepted  int32 [requests]: how many (0 for a request without rows).  d_next: int32 [requests] (-1 then).
+ * A path ends at accepted_stride rows (>= 1): the last of them is treated as one without children.  Asynchronous.
+ */
+int tl_tree_verify(const float* d_target, int64_t target_stride, const float* d_draft, int64_t draft_stride, int64_t vocab,
+                   const int32_t* d_tokens, const int32_t* d_parents, const int32_t* d_token_offsets, int requests,
+                   int tokens, const float* d_accept, const float* d_sample, int32_t* d_accepted,
+                   int64_t accepted_stride, int32_t* d_n_accepted, int32_t* d_next, void* cuda_stream);
+
 /* --------------------------------------------------- read amplification */
 
 /*

@@ -62,6 +62,13 @@ _SIGNATURES = {
     "tl_read_amp": (_int, [_i64, _i64, _i64, _int, _int, _int, _int, _i64, _int, _int, _int, _u64p, _u64p, _u64p]),
     "tl_read_amp_grouped": (_int, [_vp, _int, _i64, _i64, _int, _int, _int, _int, _i64, _int, _int, _int,
                                    _u64p, _u64p, _u64p]),
+    "tl_kv_append": (_int, [_vp, _vp, _vp, _vp, _int, _i64, _vp]),
+    "tl_kv_read": (_int, [_vp, _vp, _vp, _vp, _int, _i64, _vp]),
+    "tl_kv_commit": (_int, [_vp, _vp, _vp, _i64, _vp, _vp, _vp]),
+    "tl_tree_mask": (_int, [_vp, _vp, _int, _int, _vp, _int, _vp]),
+    "tl_tree_attention": (_int, [_vp, _vp, _vp, _i64, _int, _vp, _int, ctypes.c_float, _vp, _i64, _vp, _vp]),
+    "tl_tree_attention_workspace_bytes": (_sz, [_vp, _vp, _int]),
+    "tl_tree_verify": (_int, [_vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _int, _int, _vp, _vp, _vp, _i64, _vp, _vp, _vp]),
     "tl_read_amp_per_cta": (_int, [_i64, _i64, _i64, _int, _int, _int, _int, _i64, _int, _int, _int, _vp, _vp, _vp]),
 }
 
@@ -438,3 +445,190 @@ def read_amp_per_cta(M: int, N: int, K: int, cta, layout: int, G: int, block_row
                      elem_bytes: int, fetched: torch.Tensor, used: torch.Tensor, stream=None):
     _check(lib().tl_read_amp_per_cta(M, N, K, cta[0], cta[1], cta[2], layout, G, block_rows, block_cols, elem_bytes,
                                      _dev_ptr(fetched), _dev_ptr(used), _stream_ptr(stream)), "tl_read_amp_per_cta")
+
+
+# ------------------------------------------------------------------ key/value cache for drafted tokens
+
+KV_BF16, KV_E4M3, KV_INT8 = 0, 1, 2
+ELEM_BF16, ELEM_F32 = 0, 1
+_KV_FORMATS = {torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_E4M3, torch.int8: KV_INT8}
+_ELEMS = {torch.bfloat16: ELEM_BF16, torch.float32: ELEM_F32}
+
+
+class KvCache(ctypes.Structure):
+    """tl_kv_cache; keeps the tensors it was made from alive."""
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("pages", _i64), ("page_stride", _i64),
+                ("head_stride", _i64), ("token_stride", _i64), ("scale_page_stride", _i64), ("scale_head_stride", _i64),
+                ("format", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32)]
+
+
+class KvBatch(ctypes.Structure):
+    """tl_kv_batch; keeps the tensors it was made from alive."""
+    _fields_ = [("page_table", _vp), ("start", _vp), ("token_offsets", _vp), ("table_stride", _i64),
+                ("requests", ctypes.c_int32), ("tokens", ctypes.c_int32)]
+
+
+def _cuda(t: torch.Tensor, name: str, dtype=None, dims=None) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name}: expected a CUDA tensor")
+    if dtype is not None and t.dtype is not dtype:
+        raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+    if dims is not None and t.dim() != dims:
+        raise ValueError(f"{name}: expected {dims} dimensions, got {t.dim()}")
+    return t
+
+
+def _int32(t: torch.Tensor, name: str, shape) -> int:
+    _cuda(t, name, torch.int32)
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def kv_cache(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None,
+             v_scale: torch.Tensor | None = None) -> KvCache:
+    """k, v: [pages, heads, page_tokens, head_dim], bf16, float8_e4m3fn or int8, the last dimension contiguous (the other
+    strides are free: a permuted [pages, page_tokens, heads, head_dim] pool serves too).  k_scale, v_scale: fp32
+    [pages, heads, page_tokens], for the 8-bit formats."""
+    _cuda(k, "k", dims=4), _cuda(v, "v", k.dtype, 4)
+    if k.dtype not in _KV_FORMATS:
+        raise ValueError(f"k: expected bf16, float8_e4m3fn or int8, got {k.dtype}")
+    if v.shape != k.shape or v.stride() != k.stride() or k.stride(3) != 1:
+        raise ValueError("k and v: expected one shape and one set of strides, the last dimension contiguous")
+    c = KvCache()
+    c.format = _KV_FORMATS[k.dtype]
+    c.pages, c.heads, c.page_tokens, c.head_dim = k.shape
+    c.k, c.v = k.data_ptr(), v.data_ptr()
+    c.page_stride, c.head_stride, c.token_stride = k.stride()[:3]
+    if c.format != KV_BF16:
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            _cuda(t, name, torch.float32, 3)
+            if tuple(t.shape) != tuple(k.shape[:3]) or t.stride() != k_scale.stride() or t.stride(2) != 1:
+                raise ValueError(f"{name}: expected [pages, heads, page_tokens], the tokens contiguous, one set of strides")
+        c.k_scale, c.v_scale = k_scale.data_ptr(), v_scale.data_ptr()
+        c.scale_page_stride, c.scale_head_stride = k_scale.stride()[:2]
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("a bf16 cache has no scales")
+    c._tensors, c._ref = (k, v, k_scale, v_scale), ctypes.byref(c)
+    return c
+
+
+def kv_batch(page_table: torch.Tensor, start: torch.Tensor, token_offsets: torch.Tensor, tokens: int) -> KvBatch:
+    """page_table: int32 [requests, n]; start: int32 [requests]; token_offsets: int32 [requests + 1]."""
+    _cuda(page_table, "page_table", torch.int32, 2)
+    n = page_table.shape[0]
+    b = KvBatch()
+    b.page_table = _int32(page_table, "page_table", page_table.shape)
+    b.start = _int32(start, "start", (n,))
+    b.token_offsets = _int32(token_offsets, "token_offsets", (n + 1,))
+    b.table_stride = page_table.shape[1]
+    b.requests, b.tokens = n, int(tokens)
+    b._tensors, b._ref = (page_table, start, token_offsets), ctypes.byref(b)
+    return b
+
+
+def _kv_rows(t: torch.Tensor, name: str, cache: KvCache, batch: KvBatch):
+    """(pointer, row stride, element type) of a step's [tokens, heads, head_dim] tensor."""
+    _cuda(t, name, dims=3)
+    if t.dtype not in _ELEMS:
+        raise ValueError(f"{name}: expected bf16 or fp32, got {t.dtype}")
+    if tuple(t.shape) != (batch.tokens, cache.heads, cache.head_dim) or t.stride(2) != 1 or \
+            (cache.heads > 1 and t.stride(1) != cache.head_dim):
+        raise ValueError(f"{name}: expected [tokens, heads, head_dim] with contiguous heads")
+    return t.data_ptr(), (t.stride(0) if batch.tokens > 1 else max(t.stride(0), cache.heads * cache.head_dim)), _ELEMS[t.dtype]
+
+
+def _kv_pair(k, v, cache, batch):
+    (kp, ks, ke), (vp, vs, ve) = _kv_rows(k, "k", cache, batch), _kv_rows(v, "v", cache, batch)
+    if ks != vs or ke != ve:
+        raise ValueError("k and v: expected one element type and one row stride")
+    return kp, vp, ke, ks
+
+
+def kv_append(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, stream=None):
+    """Quantises k, v ([tokens, heads, head_dim], bf16 or fp32; column ranges of a fused product's output serve) into the
+    cache, request b's i-th row at position start[b] + i."""
+    kp, vp, elem, stride = _kv_pair(k, v, cache, batch)
+    _check(lib().tl_kv_append(cache._ref, batch._ref, kp, vp, elem, stride, _stream_ptr(stream)), "tl_kv_append")
+
+
+def kv_read(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, stream=None):
+    """Reads the positions kv_append with the same batch writes back into k, v (bf16 or fp32)."""
+    kp, vp, elem, stride = _kv_pair(k, v, cache, batch)
+    _check(lib().tl_kv_read(cache._ref, batch._ref, kp, vp, elem, stride, _stream_ptr(stream)), "tl_kv_read")
+
+
+def kv_commit(cache: KvCache, batch: KvBatch, accepted: torch.Tensor, n_accepted: torch.Tensor,
+              new_start: torch.Tensor | None = None, stream=None):
+    """Moves the rows of accepted[b][i], i < n_accepted[b], to positions start[b] + i; new_start = start + n_accepted."""
+    _cuda(accepted, "accepted", torch.int32, 2)
+    a = _int32(accepted, "accepted", (batch.requests, accepted.shape[1]))
+    n = _int32(n_accepted, "n_accepted", (batch.requests,))
+    s = _int32(new_start, "new_start", (batch.requests,)) if new_start is not None else None
+    _check(lib().tl_kv_commit(cache._ref, batch._ref, a, accepted.shape[1], n, s, _stream_ptr(stream)), "tl_kv_commit")
+
+
+def tree_mask(parents: torch.Tensor, token_offsets: torch.Tensor, mask: torch.Tensor, stream=None):
+    """mask (int32 [tokens, words]): bit j of row i is set when token i of its request sees token j."""
+    _cuda(mask, "mask", torch.int32, 2)
+    m = _int32(mask, "mask", (parents.shape[0], mask.shape[1]))
+    _check(lib().tl_tree_mask(_int32(parents, "parents", (mask.shape[0],)),
+                              _int32(token_offsets, "token_offsets", (token_offsets.shape[0],)), token_offsets.shape[0] - 1,
+                              mask.shape[0], m, mask.shape[1], _stream_ptr(stream)), "tl_tree_mask")
+
+
+def tree_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, out: torch.Tensor, mask: torch.Tensor | None = None,
+                   scale: float | None = None, lse: torch.Tensor | None = None, stream=None):
+    """out (bf16 [tokens, q_heads, head_dim]) = attention of q over the cache, which holds the step's own rows already.
+    mask: int32 [tokens, words] (None: causal within the step's rows); scale: 1 / sqrt(head_dim) by default; lse: fp32
+    [tokens, q_heads].  Rows of q and out may be strided."""
+    for t, name in ((q, "q"), (out, "out")):
+        _cuda(t, name, torch.bfloat16, 3)
+        if t.shape[0] != batch.tokens or t.shape[2] != cache.head_dim or t.shape != q.shape or t.stride(2) != 1 or \
+                (t.shape[1] > 1 and t.stride(1) != cache.head_dim):
+            raise ValueError(f"{name}: expected [tokens, q_heads, head_dim] with contiguous heads")
+    heads, words, m = q.shape[1], 0, None
+    wide = heads * cache.head_dim
+    if mask is not None:
+        words = _cuda(mask, "mask", torch.int32, 2).shape[1]
+        m = _int32(mask, "mask", (batch.tokens, words))
+    if lse is not None and (_cuda(lse, "lse", torch.float32).shape != q.shape[:2] or not lse.is_contiguous()):
+        raise ValueError("lse: expected a contiguous [tokens, q_heads]")
+    _check(lib().tl_tree_attention(cache._ref, batch._ref, q.data_ptr(), q.stride(0) if batch.tokens > 1 else wide, heads, m,
+                                   words, cache.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
+                                   out.stride(0) if batch.tokens > 1 else wide,
+                                   lse.data_ptr() if lse is not None else None, _stream_ptr(stream)), "tl_tree_attention")
+
+
+def tree_attention_workspace_bytes(cache: KvCache, batch: KvBatch, q_heads: int) -> int:
+    return int(lib().tl_tree_attention_workspace_bytes(cache._ref, batch._ref, q_heads))
+
+
+def tree_verify(target: torch.Tensor, draft: torch.Tensor | None, tokens: torch.Tensor, parents: torch.Tensor,
+                token_offsets: torch.Tensor, accept: torch.Tensor, sample: torch.Tensor, accepted: torch.Tensor,
+                n_accepted: torch.Tensor, next_token: torch.Tensor, stream=None):
+    """Which drafts the target's distribution keeps, and the token that follows them.
+
+    target, draft: fp32 [tokens, vocab] (draft None: the drafts were chosen without chance); tokens, parents: int32
+    [tokens]; accept: fp32 [tokens] and sample: fp32 [requests], uniform in [0, 1).  Written: accepted int32 [requests, n]
+    (rows kept within the request, root first, then -1), n_accepted and next_token int32 [requests].
+    """
+    rows, vocab = _cuda(target, "target", torch.float32, 2).shape
+    requests = token_offsets.shape[0] - 1
+    if draft is not None and _cuda(draft, "draft", torch.float32, 2).shape != target.shape:
+        raise ValueError("draft: expected the shape of target")
+    for t, name in ((target, "target"), (draft, "draft")):
+        if t is not None and t.stride(1) != 1 and vocab > 1:
+            raise ValueError(f"{name}: expected contiguous rows")
+    for t, name, n in ((accept, "accept", rows), (sample, "sample", requests)):
+        if _cuda(t, name, torch.float32).shape != (n,) or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous tensor of {n} numbers")
+    _cuda(accepted, "accepted", torch.int32, 2)
+    _check(lib().tl_tree_verify(target.data_ptr(), max(target.stride(0), vocab), draft.data_ptr() if draft is not None else None,
+                                max(draft.stride(0), vocab) if draft is not None else 0, vocab,
+                                _int32(tokens, "tokens", (rows,)), _int32(parents, "parents", (rows,)),
+                                _int32(token_offsets, "token_offsets", (requests + 1,)), requests, rows, accept.data_ptr(),
+                                sample.data_ptr(), _int32(accepted, "accepted", (requests, accepted.shape[1])),
+                                accepted.shape[1], _int32(n_accepted, "n_accepted", (requests,)),
+                                _int32(next_token, "next_token", (requests,)), _stream_ptr(stream)), "tl_tree_verify")

@@ -1,0 +1,152 @@
+// tl_tree_attention: argument checks, the choice of kernel, and the kernel that joins the parts of split sequences.
+#include "tl_attend.cuh"
+
+#include <algorithm>
+#include <cmath>
+
+namespace tl {
+
+// Joins the units that cross a border between CTA ranges.  Block c looks at the border in front of CTA c + 1; the
+// borders inside one unit share its rows out among themselves.
+constexpr int kCombineThreads = 256;
+__global__ void __launch_bounds__(kCombineThreads) attend_combine_kernel(const AttendParams p, int dim) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int64_t total = attend_total(p);
+    const int64_t per = attend_per_cta(total, p.ctas);
+    const int64_t border = (int64_t(blockIdx.x) + 1) * per;
+    if (border >= total) return;
+    const AttendPlace w = attend_locate(p, border);
+    if (w.tile == 0) return;                                  // the border lies between two units
+    const int64_t u0 = border - w.tile, u1 = u0 + w.a.tiles;
+    const int c0 = int(u0 / per), c1 = int((u1 - 1) / per);
+    const int share = int(blockIdx.x) - c0, shares = c1 - c0;
+    const int rows = min(p.rows_block, w.a.r.n * p.group - w.block * p.rows_block);
+    const int vecs = dim / 4;
+    for (int e = share * kCombineThreads + threadIdx.x; e < rows * vecs; e += shares * kCombineThreads) {
+        const int r = e / vecs, d = e % vecs * 4;
+        // CTA c0 ends inside the unit it began (its second slot); the others begin inside it (their first)
+        auto slot = [&](int c) { return int64_t(c) * 2 + (c == c0 ? 1 : 0); };
+        float top = -INFINITY;
+#pragma unroll 4
+        for (int c = c0; c <= c1; ++c) top = fmaxf(top, p.part_ml[slot(c) * p.rows_block + r].x);
+        const float use = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int c = c0; c <= c1; ++c) {
+            const float2 ml = p.part_ml[slot(c) * p.rows_block + r];
+            const float4 v = *reinterpret_cast<const float4*>(p.part + (slot(c) * p.rows_block + r) * dim + d);
+            const float f = ex2(ml.x - use);
+            sum = fmaf(ml.y, f, sum);
+            o.x = fmaf(v.x, f, o.x), o.y = fmaf(v.y, f, o.y), o.z = fmaf(v.z, f, o.z), o.w = fmaf(v.w, f, o.w);
+        }
+        const int row = w.block * p.rows_block + r, tok = row / p.group, hq = w.head * p.group + row % p.group;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        *reinterpret_cast<uint2*>(p.out + int64_t(w.a.r.first + tok) * p.out_stride + int64_t(hq) * dim + d) =
+            make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        if (p.lse && d == 0) p.lse[int64_t(w.a.r.first + tok) * p.q_heads + hq] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+    }
+}
+
+int attend_small_bf16(bool, int, int, int*, int*, const AttendParams*, int, cudaStream_t);
+int attend_small_e4m3(bool, int, int, int*, int*, const AttendParams*, int, cudaStream_t);
+int attend_small_int8(bool, int, int, int*, int*, const AttendParams*, int, cudaStream_t);
+static auto attend_small_of(int format) {
+    return format == TL_KV_BF16 ? attend_small_bf16 : format == TL_KV_E4M3 ? attend_small_e4m3 : attend_small_int8;
+}
+
+// Which kernel a call runs, from what the host knows: the query rows per key/value head of an average request.
+static int attend_plan(const tl_kv_cache* cache, const tl_kv_batch* batch, int q_heads, AttendPlan* plan) {
+    const int group = q_heads / cache->heads;
+    const int64_t rows = ceil_div(batch->tokens, batch->requests) * group;
+    plan->mma_rows = rows > 16 && cache->head_dim <= 128 ? 32 : 16;
+    if (int rc = attend_small_of(cache->format)(false, cache->head_dim, plan->mma_rows, &plan->tile_tokens, &plan->ctas_per_sm, nullptr, 0, nullptr)) return rc;
+    // no more CTAs than there can be tiles (the length is bounded by the page table)
+    const int64_t tiles = ceil_div(batch->table_stride * cache->page_tokens, plan->tile_tokens);
+    const int64_t units = (ceil_div(int64_t(batch->tokens) * group, plan->mma_rows) + batch->requests) * cache->heads;
+    int64_t ctas = int64_t(dev().sm_count) * plan->ctas_per_sm;
+    if (tiles < ctas && units < ctas) ctas = std::min(ctas, tiles * units);
+    plan->ctas = int(ctas);
+    const bool split = plan->ctas > 1 && tiles > 1;
+    plan->part_bytes = split ? size_t(2) * plan->ctas * plan->mma_rows * cache->head_dim * sizeof(float) : 0;
+    plan->ml_bytes = split ? size_t(2) * plan->ctas * plan->mma_rows * sizeof(float2) : 0;
+    return TL_OK;
+}
+
+static int attend_check(const tl_kv_cache* cache, const tl_kv_batch* batch, int q_heads, AttendParams* p) {
+    if (int rc = kv_view(cache, &p->cache)) return rc;
+    if (int rc = kv_batch_view(batch, &p->batch)) return rc;
+    if (q_heads < 1 || q_heads % cache->heads) return TL_ERR_INVALID_ARG;
+    if (int64_t(batch->tokens) * q_heads > INT32_MAX / 2) return TL_ERR_UNSUPPORTED;
+    return TL_OK;
+}
+
+}  // namespace tl
+
+extern "C" {
+
+size_t tl_tree_attention_workspace_bytes(const tl_kv_cache* cache, const tl_kv_batch* batch, int q_heads) {
+    using namespace tl;
+    AttendParams p = {};
+    if (attend_check(cache, batch, q_heads, &p) || batch->requests == 0 || batch->tokens == 0) return 0;
+    ApiLock lock;
+    if (ensure_device_info()) return 0;
+    AttendPlan plan = {};
+    if (attend_plan(cache, batch, q_heads, &plan)) return 0;
+    return plan.part_bytes + plan.ml_bytes;
+}
+
+int tl_tree_attention(const tl_kv_cache* cache, const tl_kv_batch* batch, const void* d_q, int64_t q_stride, int q_heads,
+                      const uint32_t* d_mask, int mask_words, float scale, void* d_out, int64_t out_stride, float* d_lse,
+                      void* cuda_stream) {
+    using namespace tl;
+    AttendParams p = {};
+    if (int rc = attend_check(cache, batch, q_heads, &p)) return rc;
+    if (d_mask && mask_words < 1) return TL_ERR_INVALID_ARG;
+    if (!std::isfinite(scale)) return TL_ERR_INVALID_ARG;
+    if (batch->requests == 0 || batch->tokens == 0) return TL_OK;
+    const int64_t wide = int64_t(q_heads) * cache->head_dim;
+    if (!d_q || !d_out || q_stride < wide || out_stride < wide) return TL_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(d_q) % 16 || reinterpret_cast<uintptr_t>(d_out) % 16 || q_stride % 8 || out_stride % 8 ||
+        reinterpret_cast<uintptr_t>(d_mask) % 4 || reinterpret_cast<uintptr_t>(d_lse) % 4)
+        return TL_ERR_ALIGNMENT;
+    if (opt(TL_OPT_PLAN_AS_IF_SMS)) return TL_ERR_INVALID_ARG;
+    ApiLock lock;
+    if (int rc = ensure_control()) return rc;
+    AttendPlan plan = {};
+    if (int rc = attend_plan(cache, batch, q_heads, &plan)) return rc;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    void* ws = nullptr;
+    if (int rc = get_workspace(plan.part_bytes + plan.ml_bytes, &ws, stream)) return rc;
+    p.q = static_cast<const __nv_bfloat16*>(d_q);
+    p.out = static_cast<__nv_bfloat16*>(d_out);
+    p.lse = d_lse;
+    p.mask = d_mask;
+    p.mask_words = mask_words;
+    p.q_stride = q_stride;
+    p.out_stride = out_stride;
+    p.group = q_heads / cache->heads;
+    p.q_heads = q_heads;
+    p.rows_block = plan.mma_rows;
+    p.tile_tokens = plan.tile_tokens;
+    p.ctas = plan.ctas;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.part = static_cast<float*>(ws);
+    p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + plan.part_bytes);
+    p.status = dev().ctl.d_status;
+    if (int rc = attend_small_of(cache->format)(true, cache->head_dim, plan.mma_rows, nullptr, nullptr, &p, plan.ctas, stream)) return rc;
+    if (plan.part_bytes == 0) return TL_OK;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(plan.ctas - 1));
+    cfg.blockDim = dim3(kCombineThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = opt(TL_OPT_PDL) != 0 ? 1 : 0;
+    return check_cuda(cudaLaunchKernelEx(&cfg, attend_combine_kernel, p, int(cache->head_dim)));
+}
+
+}  // extern "C"

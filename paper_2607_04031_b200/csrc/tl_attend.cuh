@@ -1,0 +1,128 @@
+// What the attention kernels share: their parameters and the division of the work.
+//
+// A unit is (request, key/value head, block of query rows); a row is (token, query head of the group).  A unit's
+// sequence is cut into tiles of `tile_tokens` positions; all tiles of all units form one line, in the order request,
+// head, row block, tile, and CTA c owns the tiles [c * per, (c + 1) * per) of it.  Lengths live on the device, so every
+// CTA works its range out by itself (a warp scan over the requests).  A unit inside one CTA's range is finished there;
+// one that crosses a border leaves its parts (unnormalised sums, running maximum and sum of every row) in the
+// workspace, two slots per CTA, and the combine kernel behind adds them in the order of the CTAs: no atomics, the same
+// bits every time.
+#pragma once
+
+#include "tl_kv.cuh"
+
+namespace tl {
+
+struct AttendParams {
+    KvView cache;
+    KvBatchView batch;
+    const __nv_bfloat16* q;
+    __nv_bfloat16* out;
+    float* lse;
+    const uint32_t* mask;
+    int64_t q_stride, out_stride;        // elements
+    int mask_words;
+    int group, q_heads;
+    int rows_block, tile_tokens, ctas;
+    float scale_log2;                    // scale * log2(e)
+    float* part;                         // [2 * ctas][rows_block][dim]
+    float2* part_ml;                     // [2 * ctas][rows_block]: maximum (log2 units) and sum
+    uint32_t* status;
+};
+
+#ifdef __CUDACC__
+
+struct AttendRequest {
+    KvRequest r;
+    int64_t len;                         // positions that exist
+    int row_blocks;
+    int64_t tiles;                       // per unit
+};
+__device__ __forceinline__ AttendRequest attend_request(const AttendParams& p, int b) {
+    AttendRequest a;
+    a.r = kv_request(p.batch, p.cache.page_shift, b);
+    const int64_t room = p.batch.table_stride << p.cache.page_shift;
+    a.len = min(a.r.start + a.r.n, room);
+    a.row_blocks = int((int64_t(a.r.n) * p.group + p.rows_block - 1) / p.rows_block);
+    a.tiles = (a.len + p.tile_tokens - 1) / p.tile_tokens;
+    return a;
+}
+__device__ __forceinline__ int64_t attend_request_tiles(const AttendParams& p, int b) {
+    if (b >= p.batch.requests) return 0;
+    const AttendRequest a = attend_request(p, b);
+    return a.tiles * a.row_blocks * p.cache.heads;
+}
+
+// Whole warp: the line's length.
+__device__ __forceinline__ int64_t attend_total(const AttendParams& p) {
+    int64_t sum = 0;
+    for (int b = int(lane_id()); b < p.batch.requests; b += 32) sum += attend_request_tiles(p, b);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    return sum;
+}
+__device__ __forceinline__ int64_t attend_per_cta(int64_t total, int ctas) { return (total + ctas - 1) / ctas; }
+
+struct AttendPlace {
+    int b, head, block;
+    int64_t tile;
+    AttendRequest a;
+};
+// Whole warp: where tile x of the line (x < total) lies.
+__device__ __forceinline__ AttendPlace attend_locate(const AttendParams& p, int64_t x) {
+    AttendPlace w;
+    int64_t before = 0;
+    for (int b0 = 0;; b0 += 32) {
+        const int64_t mine = attend_request_tiles(p, b0 + int(lane_id()));
+        int64_t run = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t up = __shfl_up_sync(0xffffffffu, run, d);
+            if (int(lane_id()) >= d) run += up;
+        }
+        const uint32_t past = __ballot_sync(0xffffffffu, before + run > x);
+        if (past) {
+            const int l = __ffs(int(past)) - 1;
+            w.b = b0 + l;
+            before += __shfl_sync(0xffffffffu, run - mine, l);
+            break;
+        }
+        before += __shfl_sync(0xffffffffu, run, 31);
+    }
+    w.a = attend_request(p, w.b);
+    int64_t y = x - before;
+    w.tile = y % w.a.tiles;
+    y /= w.a.tiles;
+    w.block = int(y % w.a.row_blocks);
+    w.head = int(y / w.a.row_blocks);
+    return w;
+}
+// The first tile of the next unit; the caller knows that there is one.
+__device__ __forceinline__ void attend_next_unit(const AttendParams& p, AttendPlace& w) {
+    w.tile = 0;
+    if (++w.block < w.a.row_blocks) return;
+    w.block = 0;
+    if (++w.head < p.cache.heads) return;
+    w.head = 0;
+    do {
+        w.a = attend_request(p, ++w.b);
+    } while (w.a.r.n == 0 && w.b + 1 < p.batch.requests);
+}
+
+// Whether the row's token (its place `tok` among the request's) sees token j of the step.
+__device__ __forceinline__ bool attend_sees(const AttendParams& p, int row_of_token, int tok, int64_t j) {
+    if (j < 0) return true;
+    if (!p.mask) return j <= tok;
+    if (j >= int64_t(p.mask_words) * 32) return false;
+    return (p.mask[int64_t(row_of_token) * p.mask_words + (j >> 5)] >> (j & 31)) & 1u;
+}
+
+#endif  // __CUDACC__
+
+struct AttendPlan {                      // host
+    int mma_rows;                        // query rows of a unit
+    int tile_tokens, ctas_per_sm, ctas;
+    size_t part_bytes, ml_bytes;
+};
+
+}  // namespace tl
