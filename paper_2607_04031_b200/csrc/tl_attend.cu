@@ -19,7 +19,7 @@ __global__ void __launch_bounds__(kCombineThreads) attend_combine_kernel(const A
     const AttendPlace w = attend_locate(p, border);
     if (w.tile == 0) return;                                  // the border lies between two units
     const int64_t u0 = border - w.tile, u1 = u0 + w.a.tiles;
-    const int c0 = int(u0 / per), c1 = int((u1 - 1) / per);
+    const int c0 = int(attend_div(u0, per)), c1 = int(attend_div(u1 - 1, per));
     const int share = int(blockIdx.x) - c0, shares = c1 - c0;
     const int rows = min(p.rows_block, w.a.r.n * p.group - w.block * p.rows_block);
     const int vecs = dim / 4;
@@ -56,12 +56,25 @@ static auto attend_small_of(int format) {
     return format == TL_KV_BF16 ? attend_small_bf16 : format == TL_KV_E4M3 ? attend_small_e4m3 : attend_small_int8;
 }
 
+int attend_tc_bf16(int, int, const tl_kv_cache*, const AttendParams&, cudaStream_t);
+int attend_tc_e4m3(int, int, const tl_kv_cache*, const AttendParams&, cudaStream_t);
+int attend_tc_int8(int, int, const tl_kv_cache*, const AttendParams&, cudaStream_t);
+static auto attend_tc_of(int format) {
+    return format == TL_KV_BF16 ? attend_tc_bf16 : format == TL_KV_E4M3 ? attend_tc_e4m3 : attend_tc_int8;
+}
+
 // Which kernel a call runs, from what the host knows: the query rows per key/value head of an average request.
 static int attend_plan(const tl_kv_cache* cache, const tl_kv_batch* batch, int q_heads, AttendPlan* plan) {
     const int group = q_heads / cache->heads;
     const int64_t rows = ceil_div(batch->tokens, batch->requests) * group;
-    plan->mma_rows = rows > 16 && cache->head_dim <= 128 ? 32 : 16;
-    if (int rc = attend_small_of(cache->format)(false, cache->head_dim, plan->mma_rows, &plan->tile_tokens, &plan->ctas_per_sm, nullptr, 0, nullptr)) return rc;
+    if (rows > 32 && cache->head_dim <= 128) {
+        plan->mma_rows = rows > 128 ? 256 : 128;
+        plan->tile_tokens = 128;
+        plan->ctas_per_sm = 1;
+    } else {
+        plan->mma_rows = rows > 16 && cache->head_dim <= 128 ? 32 : 16;
+        if (int rc = attend_small_of(cache->format)(false, cache->head_dim, plan->mma_rows, &plan->tile_tokens, &plan->ctas_per_sm, nullptr, 0, nullptr)) return rc;
+    }
     // no more CTAs than there can be tiles (the length is bounded by the page table)
     const int64_t tiles = ceil_div(batch->table_stride * cache->page_tokens, plan->tile_tokens);
     const int64_t units = (ceil_div(int64_t(batch->tokens) * group, plan->mma_rows) + batch->requests) * cache->heads;
@@ -129,13 +142,17 @@ int tl_tree_attention(const tl_kv_cache* cache, const tl_kv_batch* batch, const 
     p.group = q_heads / cache->heads;
     p.q_heads = q_heads;
     p.rows_block = plan.mma_rows;
-    p.tile_tokens = plan.tile_tokens;
+    for (p.rows_shift = 0; (1 << p.rows_shift) < plan.mma_rows; ++p.rows_shift) {}
+    for (p.tile_shift = 0; (1 << p.tile_shift) < plan.tile_tokens; ++p.tile_shift) {}
     p.ctas = plan.ctas;
     p.scale_log2 = scale * 1.4426950408889634f;
     p.part = static_cast<float*>(ws);
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + plan.part_bytes);
     p.status = dev().ctl.d_status;
-    if (int rc = attend_small_of(cache->format)(true, cache->head_dim, plan.mma_rows, nullptr, nullptr, &p, plan.ctas, stream)) return rc;
+    if (int rc = plan.mma_rows >= 128
+                     ? attend_tc_of(cache->format)(cache->head_dim, plan.mma_rows / 128, cache, p, stream)
+                     : attend_small_of(cache->format)(true, cache->head_dim, plan.mma_rows, nullptr, nullptr, &p, plan.ctas, stream))
+        return rc;
     if (plan.part_bytes == 0) return TL_OK;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(plan.ctas - 1));

@@ -1,7 +1,7 @@
 // What the attention kernels share: their parameters and the division of the work.
 //
 // A unit is (request, key/value head, block of query rows); a row is (token, query head of the group).  A unit's
-// sequence is cut into tiles of `tile_tokens` positions; all tiles of all units form one line, in the order request,
+// sequence is cut into tiles of 2^tile_shift positions; all tiles of all units form one line, in the order request,
 // head, row block, tile, and CTA c owns the tiles [c * per, (c + 1) * per) of it.  Lengths live on the device, so every
 // CTA works its range out by itself (a warp scan over the requests).  A unit inside one CTA's range is finished there;
 // one that crosses a border leaves its parts (unnormalised sums, running maximum and sum of every row) in the
@@ -23,7 +23,8 @@ struct AttendParams {
     int64_t q_stride, out_stride;        // elements
     int mask_words;
     int group, q_heads;
-    int rows_block, tile_tokens, ctas;
+    int rows_block, rows_shift;          // query rows of a unit, a power of two
+    int tile_shift, ctas;                // positions of a tile, a power of two
     float scale_log2;                    // scale * log2(e)
     float* part;                         // [2 * ctas][rows_block][dim]
     float2* part_ml;                     // [2 * ctas][rows_block]: maximum (log2 units) and sum
@@ -36,21 +37,21 @@ struct AttendRequest {
     KvRequest r;
     int64_t len;                         // positions that exist
     int row_blocks;
-    int64_t tiles;                       // per unit
+    int tiles;                           // per unit
 };
 __device__ __forceinline__ AttendRequest attend_request(const AttendParams& p, int b) {
     AttendRequest a;
     a.r = kv_request(p.batch, p.cache.page_shift, b);
     const int64_t room = p.batch.table_stride << p.cache.page_shift;
     a.len = min(a.r.start + a.r.n, room);
-    a.row_blocks = int((int64_t(a.r.n) * p.group + p.rows_block - 1) / p.rows_block);
-    a.tiles = (a.len + p.tile_tokens - 1) / p.tile_tokens;
+    a.row_blocks = (a.r.n * p.group + p.rows_block - 1) >> p.rows_shift;
+    a.tiles = int((a.len + (1 << p.tile_shift) - 1) >> p.tile_shift);
     return a;
 }
 __device__ __forceinline__ int64_t attend_request_tiles(const AttendParams& p, int b) {
     if (b >= p.batch.requests) return 0;
     const AttendRequest a = attend_request(p, b);
-    return a.tiles * a.row_blocks * p.cache.heads;
+    return int64_t(a.tiles) * a.row_blocks * p.cache.heads;
 }
 
 // Whole warp: the line's length.
@@ -61,11 +62,16 @@ __device__ __forceinline__ int64_t attend_total(const AttendParams& p) {
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     return sum;
 }
-__device__ __forceinline__ int64_t attend_per_cta(int64_t total, int ctas) { return (total + ctas - 1) / ctas; }
+// Quotient of numbers that are nearly always below 2^32: the 64-bit division is an order slower.
+__device__ __forceinline__ int64_t attend_div(int64_t a, int64_t b) {
+    if (((a | b) >> 32) == 0) return int64_t(uint32_t(a) / uint32_t(b));
+    return a / b;
+}
+__device__ __forceinline__ int64_t attend_per_cta(int64_t total, int ctas) { return attend_div(total + ctas - 1, ctas); }
 
 struct AttendPlace {
     int b, head, block;
-    int64_t tile;
+    int tile;
     AttendRequest a;
 };
 // Whole warp: where tile x of the line (x < total) lies.
@@ -90,11 +96,10 @@ __device__ __forceinline__ AttendPlace attend_locate(const AttendParams& p, int6
         before += __shfl_sync(0xffffffffu, run, 31);
     }
     w.a = attend_request(p, w.b);
-    int64_t y = x - before;
-    w.tile = y % w.a.tiles;
-    y /= w.a.tiles;
-    w.block = int(y % w.a.row_blocks);
-    w.head = int(y / w.a.row_blocks);
+    const int64_t y = x - before, unit = attend_div(y, w.a.tiles);
+    w.tile = int(y - unit * w.a.tiles);
+    w.head = int(uint32_t(unit) / uint32_t(w.a.row_blocks));             // (units of a request: heads x row blocks < 2^31)
+    w.block = int(unit) - w.head * w.a.row_blocks;
     return w;
 }
 // The first tile of the next unit; the caller knows that there is one.

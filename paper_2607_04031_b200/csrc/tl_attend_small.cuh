@@ -79,7 +79,7 @@ attend_kernel(const AttendParams p) {
     AttendPlace w = attend_locate(p, x);
 
     while (true) {
-        const int64_t t0 = w.tile, t1 = min(w.a.tiles, t0 + (x_end - x));
+        const int t0 = w.tile, t1 = int(min(int64_t(w.a.tiles), t0 + (x_end - x)));
         const int rows = min(S::kRows, w.a.r.n * p.group - w.block * S::kRows);
         const int32_t* const table = p.batch.page_table + int64_t(w.b) * p.batch.table_stride;
         const char* const k_head = p.cache.base[0] + int64_t(w.head) * p.cache.head_stride;
@@ -88,7 +88,7 @@ attend_kernel(const AttendParams p) {
         const int pos_mask = (1 << p.cache.page_shift) - 1;
 
         // this warp's sub-tiles: positions (t0 + i) * kTile + warp * 16, for i = 0 .. count - 1 (those that begin inside)
-        const int64_t pos_first = t0 * S::kTile + warp * 16;
+        const int64_t pos_first = int64_t(t0) * S::kTile + warp * 16;
         int64_t count64 = t1 - t0;
         if (pos_first + (count64 - 1) * S::kTile >= len) --count64;      // only the unit's last tile can begin past the end
         const int count = int(count64);

@@ -1,0 +1,8 @@
+// Instances of the tensor-core attention kernel over a bf16 cache.
+#include "tl_attend_tc_inst.cuh"
+
+namespace tl {
+int attend_tc_bf16(int dim, int blocks, const tl_kv_cache* cache, const AttendParams& p, cudaStream_t stream) {
+    return attend_tc<TL_KV_BF16>(dim, blocks, cache, p, stream);
+}
+}  // namespace tl
