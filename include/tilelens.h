@@ -497,7 +497,7 @@ typedef struct tl_kv_cache {
  * of the pool.  All four arrays are read on the device, so a captured step follows their contents.  A position past
  * the table or a page number outside [0, pages) is never touched: the row is not written / not attended to / reads
  * back as zeros, and tl_device_status() reports it (TL_ERR_TIMEOUT, detail 0xA00).  Only the table's entries that
- * hold a request's tokens are read.
+ * hold a request's tokens are read.  A sequence has at most 2^30 positions.
  */
 typedef struct tl_kv_batch {
     const int32_t* page_table;      /* device [requests][table_stride] */

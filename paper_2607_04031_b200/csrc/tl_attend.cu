@@ -12,14 +12,14 @@ constexpr int kCombineThreads = 256;
 __global__ void __launch_bounds__(kCombineThreads) attend_combine_kernel(const AttendParams p, int dim) {
     pdl_wait();
     pdl_launch_dependents();
-    const int64_t total = attend_total(p);
-    const int64_t per = attend_per_cta(total, p.ctas);
-    const int64_t border = (int64_t(blockIdx.x) + 1) * per;
-    if (border >= total) return;
+    const int total = attend_total(p), per = attend_per_cta(total, p.ctas);
+    const int64_t border64 = (int64_t(blockIdx.x) + 1) * per;
+    if (border64 >= total) return;
+    const int border = int(border64);
     const AttendPlace w = attend_locate(p, border);
     if (w.tile == 0) return;                                  // the border lies between two units
-    const int64_t u0 = border - w.tile, u1 = u0 + w.a.tiles;
-    const int c0 = int(attend_div(u0, per)), c1 = int(attend_div(u1 - 1, per));
+    const int u0 = border - w.tile, u1 = u0 + w.a.tiles;
+    const int c0 = int(uint32_t(u0) / uint32_t(per)), c1 = int(uint32_t(u1 - 1) / uint32_t(per));
     const int share = int(blockIdx.x) - c0, shares = c1 - c0;
     const int rows = min(p.rows_block, w.a.r.n * p.group - w.block * p.rows_block);
     const int vecs = dim / 4;
@@ -76,8 +76,9 @@ static int attend_plan(const tl_kv_cache* cache, const tl_kv_batch* batch, int q
         if (int rc = attend_small_of(cache->format)(false, cache->head_dim, plan->mma_rows, &plan->tile_tokens, &plan->ctas_per_sm, nullptr, 0, nullptr)) return rc;
     }
     // no more CTAs than there can be tiles (the length is bounded by the page table)
-    const int64_t tiles = ceil_div(batch->table_stride * cache->page_tokens, plan->tile_tokens);
+    const int64_t tiles = ceil_div(std::min(batch->table_stride * cache->page_tokens, kKvMaxTokens), plan->tile_tokens);
     const int64_t units = (ceil_div(int64_t(batch->tokens) * group, plan->mma_rows) + batch->requests) * cache->heads;
+    if (double(tiles) * double(units) >= double(INT32_MAX)) return TL_ERR_UNSUPPORTED;
     int64_t ctas = int64_t(dev().sm_count) * plan->ctas_per_sm;
     if (tiles < ctas && units < ctas) ctas = std::min(ctas, tiles * units);
     plan->ctas = int(ctas);

@@ -35,39 +35,31 @@ struct AttendParams {
 
 struct AttendRequest {
     KvRequest r;
-    int64_t len;                         // positions that exist
     int row_blocks;
     int tiles;                           // per unit
 };
 __device__ __forceinline__ AttendRequest attend_request(const AttendParams& p, int b) {
     AttendRequest a;
     a.r = kv_request(p.batch, p.cache.page_shift, b);
-    const int64_t room = p.batch.table_stride << p.cache.page_shift;
-    a.len = min(a.r.start + a.r.n, room);
     a.row_blocks = (a.r.n * p.group + p.rows_block - 1) >> p.rows_shift;
-    a.tiles = int((a.len + (1 << p.tile_shift) - 1) >> p.tile_shift);
+    a.tiles = (a.r.len + (1 << p.tile_shift) - 1) >> p.tile_shift;
     return a;
 }
-__device__ __forceinline__ int64_t attend_request_tiles(const AttendParams& p, int b) {
+__device__ __forceinline__ int attend_request_tiles(const AttendParams& p, int b) {
     if (b >= p.batch.requests) return 0;
     const AttendRequest a = attend_request(p, b);
-    return int64_t(a.tiles) * a.row_blocks * p.cache.heads;
+    return a.tiles * a.row_blocks * p.cache.heads;
 }
 
-// Whole warp: the line's length.
-__device__ __forceinline__ int64_t attend_total(const AttendParams& p) {
-    int64_t sum = 0;
+// Whole warp: the line's length (the host refuses batches that could have 2^31 tiles or more).
+__device__ __forceinline__ int attend_total(const AttendParams& p) {
+    int sum = 0;
     for (int b = int(lane_id()); b < p.batch.requests; b += 32) sum += attend_request_tiles(p, b);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     return sum;
 }
-// Quotient of numbers that are nearly always below 2^32: the 64-bit division is an order slower.
-__device__ __forceinline__ int64_t attend_div(int64_t a, int64_t b) {
-    if (((a | b) >> 32) == 0) return int64_t(uint32_t(a) / uint32_t(b));
-    return a / b;
-}
-__device__ __forceinline__ int64_t attend_per_cta(int64_t total, int ctas) { return attend_div(total + ctas - 1, ctas); }
+__device__ __forceinline__ int attend_per_cta(int total, int ctas) { return int(uint32_t(total + ctas - 1) / uint32_t(ctas)); }
 
 struct AttendPlace {
     int b, head, block;
@@ -75,15 +67,15 @@ struct AttendPlace {
     AttendRequest a;
 };
 // Whole warp: where tile x of the line (x < total) lies.
-__device__ __forceinline__ AttendPlace attend_locate(const AttendParams& p, int64_t x) {
+__device__ __forceinline__ AttendPlace attend_locate(const AttendParams& p, int x) {
     AttendPlace w;
-    int64_t before = 0;
+    int before = 0;
     for (int b0 = 0;; b0 += 32) {
-        const int64_t mine = attend_request_tiles(p, b0 + int(lane_id()));
-        int64_t run = mine;
+        const int mine = attend_request_tiles(p, b0 + int(lane_id()));
+        int run = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int64_t up = __shfl_up_sync(0xffffffffu, run, d);
+            const int up = __shfl_up_sync(0xffffffffu, run, d);
             if (int(lane_id()) >= d) run += up;
         }
         const uint32_t past = __ballot_sync(0xffffffffu, before + run > x);
@@ -96,10 +88,10 @@ __device__ __forceinline__ AttendPlace attend_locate(const AttendParams& p, int6
         before += __shfl_sync(0xffffffffu, run, 31);
     }
     w.a = attend_request(p, w.b);
-    const int64_t y = x - before, unit = attend_div(y, w.a.tiles);
-    w.tile = int(y - unit * w.a.tiles);
-    w.head = int(uint32_t(unit) / uint32_t(w.a.row_blocks));             // (units of a request: heads x row blocks < 2^31)
-    w.block = int(unit) - w.head * w.a.row_blocks;
+    const uint32_t y = uint32_t(x - before), unit = y / uint32_t(w.a.tiles), head = unit / uint32_t(w.a.row_blocks);
+    w.tile = int(y - unit * uint32_t(w.a.tiles));
+    w.head = int(head);
+    w.block = int(unit - head * uint32_t(w.a.row_blocks));
     return w;
 }
 // The first tile of the next unit; the caller knows that there is one.
@@ -115,10 +107,10 @@ __device__ __forceinline__ void attend_next_unit(const AttendParams& p, AttendPl
 }
 
 // Whether the row's token (its place `tok` among the request's) sees token j of the step.
-__device__ __forceinline__ bool attend_sees(const AttendParams& p, int row_of_token, int tok, int64_t j) {
+__device__ __forceinline__ bool attend_sees(const AttendParams& p, int row_of_token, int tok, int j) {
     if (j < 0) return true;
     if (!p.mask) return j <= tok;
-    if (j >= int64_t(p.mask_words) * 32) return false;
+    if ((j >> 5) >= p.mask_words) return false;
     return (p.mask[int64_t(row_of_token) * p.mask_words + (j >> 5)] >> (j & 31)) & 1u;
 }
 

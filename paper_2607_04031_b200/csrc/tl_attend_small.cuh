@@ -71,31 +71,28 @@ attend_kernel(const AttendParams p) {
 
     pdl_wait();
     pdl_launch_dependents();
-    const int64_t total = attend_total(p);
-    const int64_t per = attend_per_cta(total, p.ctas);
-    int64_t x = int64_t(blockIdx.x) * per;
-    const int64_t x_end = min(x + per, total);
+    const int total = attend_total(p), per = attend_per_cta(total, p.ctas);
+    int x = int(min(int64_t(blockIdx.x) * per, int64_t(total)));
+    const int x_end = x + min(per, total - x);
     if (x >= x_end) return;
     AttendPlace w = attend_locate(p, x);
 
     while (true) {
-        const int t0 = w.tile, t1 = int(min(int64_t(w.a.tiles), t0 + (x_end - x)));
+        const int t0 = w.tile, t1 = min(w.a.tiles, t0 + (x_end - x));
         const int rows = min(S::kRows, w.a.r.n * p.group - w.block * S::kRows);
         const int32_t* const table = p.batch.page_table + int64_t(w.b) * p.batch.table_stride;
         const char* const k_head = p.cache.base[0] + int64_t(w.head) * p.cache.head_stride;
         const char* const v_head = p.cache.base[1] + int64_t(w.head) * p.cache.head_stride;
-        const int64_t len = w.a.len, start = w.a.r.start;
+        const int len = w.a.r.len, start = w.a.r.start;
         const int pos_mask = (1 << p.cache.page_shift) - 1;
 
         // this warp's sub-tiles: positions (t0 + i) * kTile + warp * 16, for i = 0 .. count - 1 (those that begin inside)
-        const int64_t pos_first = int64_t(t0) * S::kTile + warp * 16;
-        int64_t count64 = t1 - t0;
-        if (pos_first + (count64 - 1) * S::kTile >= len) --count64;      // only the unit's last tile can begin past the end
-        const int count = int(count64);
+        const int pos_first = t0 * S::kTile + warp * 16;
+        int count = t1 - t0;
+        if (pos_first + (count - 1) * S::kTile >= len) --count;          // only the unit's last tile can begin past the end
         auto page_of = [&](int i) -> int {                               // page number, or -1
             if (i >= count) return -1;
-            const int64_t slot = (pos_first + int64_t(i) * S::kTile) >> p.cache.page_shift;
-            const int page = table[slot];                                // (slot is inside the table: pos < len)
+            const int page = table[(pos_first + i * S::kTile) >> p.cache.page_shift];   // (slot is inside the table: pos < len)
             return page >= 0 && page < p.cache.pages ? page : -1;
         };
         // page numbers of 32 sub-tiles, one per lane, the next 32 on the way
@@ -110,9 +107,9 @@ attend_kernel(const AttendParams p) {
                 const int page = __shfl_sync(0xffffffffu, pages, i & 31);
                 const bool ok = page >= 0;
                 bad_any |= ok ? 0u : 1u;
-                const int64_t pos = pos_first + int64_t(i) * S::kTile;
-                const int line = int(pos) & pos_mask;
-                const int left = int(min(len - pos, int64_t(16)));
+                const int pos = pos_first + i * S::kTile;
+                const int line = pos & pos_mask;
+                const int left = len - pos;
                 const int64_t at = ok ? int64_t(page) * p.cache.page_stride + int64_t(line) * p.cache.token_stride : 0;
                 const uint32_t dst = ring + uint32_t((i % S::kStages) * S::kStageBytes);
 #pragma unroll
@@ -250,7 +247,7 @@ attend_kernel(const AttendParams p) {
                 }
             }
             // scores in log2 units; thread's positions: nt * 8 + 2t + {0, 1}
-            const int64_t pos0 = pos_first + int64_t(i) * S::kTile;
+            const int pos0 = pos_first + i * S::kTile;
             float rvs[2][2];
             if (!kBf16) {
                 const float* sc = reinterpret_cast<const float*>(st + 32 * S::kRowBytes);
@@ -295,7 +292,7 @@ attend_kernel(const AttendParams p) {
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const int64_t pos = pos0 + (e >> 1) * 8 + 2 * t + (e & 1);
+                            const int pos = pos0 + (e >> 1) * 8 + 2 * t + (e & 1);
                             const bool vis = ok && pos < len && attend_sees(p, w.a.r.first + tok_of[mt][h], tok_of[mt][h], pos - start);
                             if (vis) seen |= 1u << ((mt * 2 + h) * 4 + e);
                             else s[mt][e >> 1][2 * h + (e & 1)] = -INFINITY;
@@ -422,7 +419,7 @@ attend_kernel(const AttendParams p) {
         }
         cp_async_wait<0>();
         if (bad_any && lane == 0) atomicCAS(p.status, 0u, kBadPage);
-        if (w.a.r.cut && threadIdx.x == 0) atomicCAS(p.status, 0u, kBadPage);
+        if (w.a.r.n > len - start && threadIdx.x == 0) atomicCAS(p.status, 0u, kBadPage);
 
         // join the warps: a common maximum per row, then the sums
 #pragma unroll

@@ -1,22 +1,21 @@
 // Attention for many query rows per key/value head (trees, chains of drafts, prompt chunks) on the 5th-generation
 // tensor cores.
 //
-// One CTA per SM, four warpgroups: two for softmax (streams A and B), one of producers, and one whose first warp issues
-// the matrix instructions; registers are moved from the last two to the first two (168 + 168 + 120 + 56 = 4 x 128 a thread).  A stream is an accumulator O (128 rows x dim) and a score tile S (128 x 128) in tensor memory.
+// One CTA per SM, five warpgroups: two for softmax (streams A and B), two of producers, and one whose first warp issues
+// the matrix instructions; registers are moved from the last three to the first two.  A stream is an accumulator O (128 rows x dim) and a score tile S (128 x 128) in tensor memory.
 //   kBlocks = 2  the streams hold different rows (256 rows a unit) and use every key/value tile together: each fetched
 //                and converted element serves 256 rows;
 //   kBlocks = 1  the streams hold the same 128 rows and take the tiles in turn; their sums are joined at the end.
 // Either way one stream's products run while the other's softmax does.  Per tile and stream: S = Q K^T (both operands in
-// shared memory, 128-byte swizzle), thread r of the warpgroup reads row r of S (no exchange between threads), writes the
-// weights back over S as 16-bit values, and O += P V takes P from tensor memory and V from shared memory as an MN-major
+// shared memory, 128-byte swizzle), the warpgroup reads S, writes the weights back over it as 16-bit values, and O += P V takes P from tensor memory and V from shared memory as an MN-major
 // operand, so neither P nor V^T is ever laid out again.
 //
-// The row maximum is allowed to lag: weights are taken against the maximum known when the tile began, and only when a
-// score exceeds that by more than 2^8 is the tile done again with the new maximum and O rescaled; sums are fp32 and f16
-// has room for 2^15, so the lag costs no accuracy.  Scales of 8-bit caches enter as in the kernel for few rows (key's
+// The row maximum is allowed to lag: weights are taken against the maximum known so far, and only when a score exceeds
+// it by more than 2^8 are O, the sum and the tile's earlier weights rescaled; sums are fp32 and f16 has room for 2^15, so
+// the lag costs no accuracy.  Scales of 8-bit caches enter as in the kernel for few rows (key's
 // scale on the score, value's in the exponent), q is f16 scaled by a power of two per row; conversion to f16 is exact.
 //
-// 8-bit tiles are loaded by the producers into registers one tile ahead, converted and stored swizzled; full bf16 tiles
+// 8-bit tiles are fetched by the producers one tile ahead, converted and stored swizzled; full bf16 tiles
 // come by TMA (128-byte-swizzled boxes, one per page and 64 dimensions); a tile with positions past the end, or with a
 // page outside the pool, goes through registers too, with zeros in those places.
 #pragma once
@@ -27,8 +26,12 @@ namespace tl {
 
 enum : uint32_t { kWaitAttend = 0xC00 };
 
-constexpr int kTcTile = 128, kTcThreads = 16 * 32;
-constexpr int kTcSoftmaxWarps = 8, kTcProducerWarp = 8, kTcMmaWarp = 12;
+constexpr int kTcTile = 128, kTcThreads = 20 * 32;
+constexpr int kTcSoftmaxWarps = 8, kTcProducerWarp = 8, kTcProducers = 8, kTcMmaWarp = 16;
+constexpr int kTcProducerThreads = kTcProducers * 32;
+// Registers per thread: the launch has 96 for each of 640 threads, 61440; 256 x 120 + 256 x 88 + 128 x 64 is as many.
+constexpr int kTcSoftmaxRegs = 120, kTcProducerRegs = 88, kTcMmaRegs = 64;
+constexpr float kTcNoMax = -3.0e38f;     // in place of a maximum while a row has seen nothing
 
 struct AttendTcParams {
     AttendParams a;
@@ -42,13 +45,17 @@ struct TcShape {
     static constexpr int kAtoms = kDim / 64;                       // 128-byte columns of a 16-bit operand tile
     static constexpr int kAtomBytes = kTcTile * 128;
     static constexpr int kOperand = kAtoms * kAtomBytes;           // one 128-row operand tile
-    static constexpr int kKStages = 2, kVStages = kBlocks == 1 ? 3 : 2;
+    static constexpr int kKStages = 2, kVStages = 2;
     static constexpr int kOffK = kBlocks * kOperand;
     static constexpr int kOffV = kOffK + kKStages * kOperand;
     static constexpr int kOffScale = kOffV + kVStages * kOperand;  // [stage][ks, log2 vs, 1 / vs][128]
     static constexpr int kOffStat = kOffScale + kVStages * 3 * kTcTile * 4;
-    static constexpr int kOffBar = kOffStat + 2 * kTcTile * 16;
-    static constexpr int kSmem = kOffBar + 256 + 1024;             // 1024: the base is aligned by hand
+    static constexpr int kOffBar = kOffStat + (kBlocks == 1 ? 2 * kTcTile * 16 : 0);
+    // 8-bit caches: codes on their way to conversion, 16 bytes per producer thread and round, one round kept in registers
+    static constexpr int kRounds = kDim / 32;                      // of 256 threads x 16 bytes, per tile of keys or values
+    static constexpr int kOffRaw = kOffBar + 256;
+    static constexpr int kRawSlots = 2 * kRounds - 1;
+    static constexpr int kSmem = kOffRaw + kRawSlots * 4096 + 1024;    // 1024: the base is aligned by hand
     static constexpr int kRows = kBlocks * 128;
     // tensor memory columns
     static constexpr int kS = 0, kO = 256;                         // S of stream x at x * 128, O at 256 + x * 128
@@ -64,31 +71,45 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* tmap, uint
         : "memory");
 }
 // D[tmem] (+)= A[tmem] * B[smem desc]
-__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+        "mov.b64 b, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st_32x32b_x32(uint32_t taddr, const uint32_t* v) {
+__device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_t (&v)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
         ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
-          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
-          "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
-          "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(taddr)
+          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr)
         : "memory");
+}
+// 16 lanes x 32 columns: thread (g = lane / 4, t = lane % 4) gets, of every 8 columns, columns 2t and 2t + 1 of lane g and
+// of lane g + 8 (4 registers).
+__device__ __forceinline__ void tmem_ld_16x256b_x4(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr)
+        : "memory");
+}
+// 16 lanes x 16 columns: of every 4 columns, thread (g, t) gives or gets column t of lane g and of lane g + 8.
+__device__ __forceinline__ void tmem_st_16x128b_x4(uint32_t taddr, const uint32_t (&v)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_16x128b_x4(uint32_t taddr, uint32_t (&v)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x128b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-// Shared-memory descriptor without its address: 128-byte swizzle, leading and stride byte offsets.
-__device__ __forceinline__ uint64_t tc_desc_hi(uint32_t lbo, uint32_t sbo) {
-    return (uint64_t(lbo >> 4) << 16) | (uint64_t(sbo >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
-}
 
 template <int kRegs>
 __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
@@ -132,7 +153,7 @@ struct TcBars {
     uint64_t drained;                    // the issuing thread's last commit, when it gives up
     uint32_t abort_flag, tmem_base;
     uint32_t meta[3];                    // per value stage: groups of 16 positions that should have a page and have none
-    uint32_t odd[3][4];                  // per value stage and producer warp: values that are not finite were taken out
+    alignas(8) uint8_t odd[3][kTcProducers];        // per value stage and producer warp: values that are not finite were taken out
 };
 static_assert(sizeof(TcBars) <= 256, "barrier block");
 
@@ -152,9 +173,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
     if (threadIdx.x == 0) {
         mbar_init(&bars.q_full, kTcSoftmaxWarps);
         for (int i = 0; i < 3; ++i) {
-            mbar_init(&bars.k_full[i], 4);
+            mbar_init(&bars.k_full[i], kTcProducers);
             mbar_init(&bars.k_empty[i], 1);
-            mbar_init(&bars.v_full[i], 4);
+            mbar_init(&bars.v_full[i], kTcProducers);
             mbar_init(&bars.v_empty[i], 1);
         }
         for (int x = 0; x < 2; ++x) {
@@ -178,33 +199,41 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
 
     pdl_wait();
     pdl_launch_dependents();
-    const int64_t total = attend_total(p);
-    const int64_t per = attend_per_cta(total, p.ctas);
-    int64_t x0 = int64_t(blockIdx.x) * per;
-    const int64_t x_end = min(x0 + per, total);
+    const int total = attend_total(p), per = attend_per_cta(total, p.ctas);
+    int x0 = int(min(int64_t(blockIdx.x) * per, int64_t(total)));
+    const int x_end = x0 + min(per, total - x0);
 
     auto wait = [&](uint64_t* bar, uint32_t parity) {
         return mbar_wait_bounded(bar, parity, abort_ptr, p.status, kWaitAttend, tp.wait_ns);
     };
     auto warp_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
 
+    // The end of every role, each with a copy of its own: a common one would have the compiler hold all of them to the
+    // smallest register share.
+    auto leave = [&]() {
+        __syncwarp();
+        tc_fence_before_sync();
+        __syncthreads();
+        tc_fence_after_sync();
+        if (warp == kTcMmaWarp) tmem_dealloc(tmem, 512);
+    };
+
     if (x0 < x_end) {
         AttendPlace w = attend_locate(p, x0);
         uint32_t tiles_before = 0;                             // tiles of this CTA's earlier units: ring positions count on
         uint32_t unit = 0;
         bool alive = true;
-
         if (warp < kTcSoftmaxWarps) {
             // ============================================================ softmax
             // (every warpgroup of a CTA with work takes its share: together they are what the block was launched with)
-            reg_inc<168>();
+            reg_inc<kTcSoftmaxRegs>();
             const int stream = warp / 4, r = int(threadIdx.x) & 127;
             const uint32_t lanes = uint32_t(warp & 3) * 32u << 16;           // this warp's quarter of tensor memory
             const uint32_t s_tmem = tmem + lanes + S::kS + uint32_t(stream) * 128u;
             const uint32_t o_tmem = tmem + lanes + S::kO + uint32_t(stream) * 128u;
             uint32_t s_count = 0;
             while (true) {
-                const int t0 = w.tile, t1 = int(min(int64_t(w.a.tiles), t0 + (x_end - x0)));
+                const int t0 = w.tile, t1 = min(w.a.tiles, t0 + (x_end - x0));
                 const int tiles = t1 - t0;
                 const int unit_rows = min(S::kRows, w.a.r.n * p.group - w.block * S::kRows);
                 const int row = w.block * S::kRows + (kBlocks == 2 ? stream * 128 : 0) + r;
@@ -213,17 +242,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 const bool active = kBlocks == 2 ? stream * 128 < unit_rows : stream < tiles;
                 float fac = p.scale_log2;
                 {
-                    // this row of q, converted, into the operand tile
-                    uint4 q[kDim / 8];
+                    // this row of q, converted, into the operand tile (twice over the row: the scale first)
                     const uint4* src = reinterpret_cast<const uint4*>(p.q + int64_t(w.a.r.first + tok) * p.q_stride + int64_t(hq) * kDim);
-#pragma unroll
-                    for (int c = 0; c < kDim / 8; ++c) q[c] = live ? src[c] : make_uint4(0, 0, 0, 0);
                     float mul = 1.0f;
                     if (!kBf16) {
                         uint32_t top = 0;
-#pragma unroll
+#pragma unroll 4
                         for (int c = 0; c < kDim / 8; ++c) {
-                            const uint32_t u[4] = {q[c].x, q[c].y, q[c].z, q[c].w};
+                            const uint4 q = __ldg(src + c);
+                            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
                             for (int i = 0; i < 4; ++i) top = max(top, max((u[i] << 16) & 0x7fff0000u, u[i] & 0x7fff0000u));
                         }
@@ -234,15 +261,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     }
                     if (kBlocks == 2 || stream == 0) {
                         char* const dst = smem + (kBlocks == 2 ? stream * S::kOperand : 0) + r * 128;
-#pragma unroll
+#pragma unroll 4
                         for (int c = 0; c < kDim / 8; ++c) {
-                            uint4 v = q[c];
+                            uint4 v = __ldg(src + c);
                             if (!kBf16) {
                                 uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) u[i] = pack_f16(__uint_as_float(u[i] << 16) * mul, __uint_as_float(u[i] & 0xffff0000u) * mul);
                                 v = make_uint4(u[0], u[1], u[2], u[3]);
                             }
+                            if (!live) v = make_uint4(0, 0, 0, 0);
                             *reinterpret_cast<uint4*>(dst + (c / 8) * S::kAtomBytes + (((c % 8) ^ (r & 7)) << 4)) = v;
                         }
                     }
@@ -252,7 +280,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars.q_full);
 
-                float m = -INFINITY, l = 0.0f;
+                // In the loop thread (g, t) holds rows g + 8h (h = 0..3) of its warp's 32 and columns 2t, 2t + 1 of every 8: the
+                // four threads of a row share it, and a column's scales are fetched by the eight threads that need them.
+                const int g = lane >> 2, t4 = lane & 3;
+                float m[4], l[4], fac4[4];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    m[h] = kTcNoMax;
+                    l[h] = 0.0f;
+                    fac4[h] = __shfl_sync(0xffffffffu, fac, g + 8 * h);
+                }
+                // from there to one row per thread, for O
+                auto to_row = [&](const float (&v)[4]) -> float {
+                    float r0 = __shfl_sync(0xffffffffu, v[0], (lane & 7) * 4), r1 = __shfl_sync(0xffffffffu, v[1], (lane & 7) * 4);
+                    float r2 = __shfl_sync(0xffffffffu, v[2], (lane & 7) * 4), r3 = __shfl_sync(0xffffffffu, v[3], (lane & 7) * 4);
+                    r0 = lane & 8 ? r1 : r0;
+                    r2 = lane & 8 ? r3 : r2;
+                    return lane & 16 ? r2 : r0;
+                };
                 bool odd = false;
                 const int step = kBlocks == 2 ? 1 : 2;
                 for (int n = kBlocks == 2 ? 0 : stream; active && n < tiles; n += step) {
@@ -264,135 +309,165 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     ++s_count;
                     tc_fence_after_sync();
                     const uint32_t meta = bars.meta[at];
-                    if (kBf16) odd |= (bars.odd[at][0] | bars.odd[at][1] | bars.odd[at][2] | bars.odd[at][3]) != 0;
-                    const int64_t pos0 = int64_t(t0 + n) * kTcTile;
+                    if (kBf16) odd |= *reinterpret_cast<const uint64_t*>(bars.odd[at]) != 0;
+                    const int pos0 = (t0 + n) * kTcTile;
                     const bool edge = pos0 + kTcTile > w.a.r.start || meta != 0;
-                    const float4* const ks = reinterpret_cast<const float4*>(scales + at * 3 * kTcTile);
-                    const float4* const lv = ks + kTcTile / 4;
-                    const float4* const rv = lv + kTcTile / 4;
-                    // bit i: this row sees position pos0 + 32 c + i
+                    const float* const ks = scales + at * 3 * kTcTile + 2 * t4;
+                    // bit i: this thread's row sees position pos0 + 32 c + i
                     auto sees32 = [&](int c) -> uint32_t {
-                        const int64_t pos = pos0 + c * 32;
-                        if (pos >= w.a.len) return 0u;
-                        uint32_t see = w.a.len - pos >= 32 ? 0xffffffffu : (1u << int(w.a.len - pos)) - 1u;
+                        const int pos = pos0 + c * 32;
+                        if (pos >= w.a.r.len) return 0u;
+                        uint32_t see = w.a.r.len - pos >= 32 ? 0xffffffffu : (1u << (w.a.r.len - pos)) - 1u;
                         if (meta & (1u << (2 * c))) see &= 0xffff0000u;
                         if (meta & (2u << (2 * c))) see &= 0x0000ffffu;
-                        const int64_t j = pos - w.a.r.start;                 // the step's token at bit 0
+                        const int j = pos - w.a.r.start;                     // the step's token at bit 0
                         if (j + 31 < 0) return see;
-                        auto word = [&](int64_t k) -> uint32_t {             // tokens 32 k .. 32 k + 31
+                        auto word = [&](int k) -> uint32_t {                 // tokens 32 k .. 32 k + 31
                             if (k < 0) return 0xffffffffu;
                             if (p.mask) return k < p.mask_words ? p.mask[int64_t(w.a.r.first + tok) * p.mask_words + k] : 0u;
-                            const int64_t d = tok - k * 32;
-                            return d >= 31 ? 0xffffffffu : d < 0 ? 0u : (2u << int(d)) - 1u;
+                            const int d = tok - k * 32;
+                            return d >= 31 ? 0xffffffffu : d < 0 ? 0u : (2u << d) - 1u;
                         };
-                        const int64_t k = j >> 5;
+                        const int k = j >> 5;
                         return see & __funnelshift_r(word(k), word(k + 1), uint32_t(j & 31));
                     };
-                    // scores of 32 columns in log2 units
-                    auto load_scores = [&](int c, F2 (&t)[16]) {
-                        uint32_t v[32];
-                        tmem_ld_32x32b_x32(s_tmem + uint32_t(c) * 32u, v);
-                        tmem_ld_wait();
-                        const F2 f = {fac, fac};
+                    // The tile goes by in four pieces of 32 columns; the weights of a piece take the place of scores that have been
+                    // read (16-bit values: half the columns).
+                    F2 sum[4];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            F2 a = {__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1])};
-                            F2 b = {__uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3])};
-                            if (kBf16) {
-                                t[2 * i] = f2_mul(a, f);
-                                t[2 * i + 1] = f2_mul(b, f);
-                            } else {
-                                const float4 k4 = ks[c * 8 + i], v4 = lv[c * 8 + i];
-                                t[2 * i] = f2_fma(f2_mul(a, F2{k4.x, k4.y}), f, F2{v4.x, v4.y});
-                                t[2 * i + 1] = f2_fma(f2_mul(b, F2{k4.z, k4.w}), f, F2{v4.z, v4.w});
+                    for (int h = 0; h < 4; ++h) sum[h] = F2{0.0f, 0.0f};
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        // scores in log2 units: d[h][i] are columns 32 c + 8 i + 2t + {0, 1} of row g + 8h
+                        F2 d[4][4];
+                        const float* const kc = ks + c * 32;
+                        {
+                            uint32_t v[2][16];
+                            tmem_ld_16x256b_x4(s_tmem + uint32_t(c) * 32u, v[0]);
+                            tmem_ld_16x256b_x4(s_tmem + (16u << 16) + uint32_t(c) * 32u, v[1]);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                F2 k2 = {1.0f, 1.0f}, v2 = {0.0f, 0.0f};
+                                if (!kBf16) {
+                                    k2 = *reinterpret_cast<const F2*>(kc + i * 8);
+                                    v2 = *reinterpret_cast<const F2*>(kc + kTcTile + i * 8);
+                                }
+#pragma unroll
+                                for (int h = 0; h < 4; ++h) {
+                                    const F2 a = {__uint_as_float(v[h >> 1][4 * i + 2 * (h & 1)]), __uint_as_float(v[h >> 1][4 * i + 2 * (h & 1) + 1])};
+                                    const F2 f = {fac4[h], fac4[h]};
+                                    d[h][i] = kBf16 ? f2_mul(a, f) : f2_fma(f2_mul(a, k2), f, v2);
+                                }
                             }
                         }
                         if (edge) {
                             const uint32_t see = sees32(c);
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                if (!(see >> (2 * i) & 1u)) t[i].x = -INFINITY;
-                                if (!(see >> (2 * i + 1) & 1u)) t[i].y = -INFINITY;
+                            for (int h = 0; h < 4; ++h) {
+                                const uint32_t s4 = __shfl_sync(0xffffffffu, see, g + 8 * h) >> (2 * t4);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    if (!(s4 >> (8 * i) & 1u)) d[h][i].x = -INFINITY;
+                                    if (!(s4 >> (8 * i) & 2u)) d[h][i].y = -INFINITY;
+                                }
                             }
                         }
-                    };
-                    uint32_t pw[64];
-                    bool fresh = __any_sync(0xffffffffu, m == -INFINITY);
-                    while (true) {
-                        if (fresh) {
-                            float top = -INFINITY;
-#pragma unroll 1
-                            for (int c = 0; c < 4; ++c) {
-                                F2 t[16];
-                                load_scores(c, t);
+                        float top[4], over = kTcNoMax;                       // how far a score lies above its row's maximum
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) top = fmaxf(top, fmaxf(t[i].x, t[i].y));
+                        for (int h = 0; h < 4; ++h) {
+                            top[h] = fmaxf(fmaxf(d[h][0].x, d[h][0].y), fmaxf(d[h][1].x, d[h][1].y));
+                            top[h] = fmaxf(top[h], fmaxf(fmaxf(d[h][2].x, d[h][2].y), fmaxf(d[h][3].x, d[h][3].y)));
+                            over = fmaxf(over, top[h] - m[h]);
+                        }
+                        if (__any_sync(0xffffffffu, over > 8.0f)) {
+                            // a new maximum: what was taken against the old one is rescaled
+                            float f[4];
+#pragma unroll
+                            for (int h = 0; h < 4; ++h) {
+                                top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
+                                top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
+                                const float m_new = fmaxf(m[h], top[h]);
+                                f[h] = ex2(m[h] - m_new);
+                                m[h] = m_new;
+                                l[h] *= f[h];
+                                sum[h] = f2_mul(sum[h], F2{f[h], f[h]});
                             }
-                            const float m_new = fmaxf(m, top);
-                            const float f = m == -INFINITY ? 0.0f : ex2(m - m_new);
-                            if (!first && __any_sync(0xffffffffu, m_new > m)) {
-                                // (S of this tile was issued after the previous O += P V had completed)
+                            tmem_st_wait();
 #pragma unroll 1
-                                for (int c = 0; c < kDim / 32; ++c) {
-                                    uint32_t v[32];
-                                    tmem_ld_32x32b_x32(o_tmem + uint32_t(c) * 32u, v);
+                            for (int k = 0; k < 2 * c; ++k) {                // this tile's weights so far
+                                const uint32_t at_p = s_tmem + uint32_t(k & 1) * (16u << 16) + uint32_t(k >> 1) * 16u;
+                                uint32_t pv[8];
+                                tmem_ld_16x128b_x4(at_p, pv);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    const float fh = k & 1 ? (i & 1 ? f[3] : f[2]) : (i & 1 ? f[1] : f[0]);
+                                    if (kBf16) {
+                                        pv[i] = pack_bf16(__uint_as_float(pv[i] << 16) * fh, __uint_as_float(pv[i] & 0xffff0000u) * fh);
+                                    } else {
+                                        const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&pv[i]));
+                                        pv[i] = pack_f16(e.x * fh, e.y * fh);
+                                    }
+                                }
+                                tmem_st_16x128b_x4(at_p, pv);
+                            }
+                            if (!first) {
+                                // (S of this tile was issued after the previous O += P V had completed)
+                                const float fr = to_row(f);
+#pragma unroll 1
+                                for (int k = 0; k < kDim / 16; ++k) {
+                                    uint32_t o[16];
+                                    tmem_ld_32x32b_x16(o_tmem + uint32_t(k) * 16u, o);
                                     tmem_ld_wait();
 #pragma unroll
-                                    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-                                    tmem_st_32x32b_x32(o_tmem + uint32_t(c) * 32u, v);
-                                }
-                            }
-                            l *= f;
-                            m = m_new;
-                        }
-                        const float use = m == -INFINITY ? 0.0f : m;
-                        const F2 minus = {-use, -use};
-                        F2 top = {-INFINITY, -INFINITY}, sum = {0.0f, 0.0f};
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            F2 t[16];
-                            load_scores(c, t);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                top.x = fmaxf(top.x, t[i].x);
-                                top.y = fmaxf(top.y, t[i].y);
-                                const F2 d = f2_add(t[i], minus);
-                                const F2 e = {ex2(d.x), ex2(d.y)};
-                                if (kBf16) {
-                                    sum = f2_add(sum, e);
-                                    pw[c * 16 + i] = pack_bf16(e.x, e.y);
-                                } else {
-                                    const float2 r2 = reinterpret_cast<const float2*>(rv)[c * 16 + i];
-                                    sum = f2_fma(e, F2{r2.x, r2.y}, sum);
-                                    pw[c * 16 + i] = pack_f16(e.x, e.y);
+                                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * fr);
+                                    tmem_st_32x32b_x16(o_tmem + uint32_t(k) * 16u, o);
                                 }
                             }
                         }
-                        if (!fresh && __any_sync(0xffffffffu, fmaxf(top.x, top.y) > use + 8.0f)) {
-                            fresh = true;
-                            continue;
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            uint32_t pw[8];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                F2 r2 = {1.0f, 1.0f};
+                                if (!kBf16) r2 = *reinterpret_cast<const F2*>(kc + 2 * kTcTile + i * 8);
+#pragma unroll
+                                for (int hh = 0; hh < 2; ++hh) {
+                                    const int h = half * 2 + hh;
+                                    const F2 x = f2_add(d[h][i], F2{-m[h], -m[h]});
+                                    const F2 e = {ex2(x.x), ex2(x.y)};
+                                    sum[h] = kBf16 ? f2_add(sum[h], e) : f2_fma(e, r2, sum[h]);
+                                    pw[2 * i + hh] = kBf16 ? pack_bf16(e.x, e.y) : pack_f16(e.x, e.y);
+                                }
+                            }
+                            tmem_st_16x128b_x4(s_tmem + uint32_t(half) * (16u << 16) + uint32_t(c) * 16u, pw);
                         }
-                        l += sum.x + sum.y;
-                        break;
                     }
-                    tmem_st_32x32b_x32(s_tmem, pw);
-                    tmem_st_32x32b_x32(s_tmem + 32u, pw + 32);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) l[h] += sum[h].x + sum[h].y;
                     tmem_st_wait();
                     tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bars.p_full[stream]);
                 }
                 if (!alive) break;
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+                    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+                }
+                const float m_row = to_row(m), l_row = to_row(l);
                 // the last product of this stream
                 if (active) {
                     alive = warp_wait(&bars.pv_done[stream], (s_count - 1) & 1u);
                     if (!alive) break;
                     tc_fence_after_sync();
                 }
-                float f_own = 1.0f, f_other = 0.0f, m_all = m, l_all = l;
+                float f_own = 1.0f, f_other = 0.0f, m_all = m_row, l_all = l_row;
                 bool odd_all = odd;
                 if (kBlocks == 1) {
-                    stats[stream * kTcTile + r] = make_float4(m, l, odd ? 1.0f : 0.0f, 0.0f);
+                    stats[stream * kTcTile + r] = make_float4(m_row, l_row, odd ? 1.0f : 0.0f, 0.0f);
                     tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bars.exchange);
@@ -400,11 +475,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     if (!alive) break;
                     tc_fence_after_sync();
                     const float4 o = stats[(stream ^ 1) * kTcTile + r];
-                    m_all = fmaxf(m, o.x);
+                    m_all = fmaxf(m_row, o.x);
                     const float use = m_all == -INFINITY ? 0.0f : m_all;
-                    f_own = ex2(m - use);
+                    f_own = ex2(m_row - use);
                     f_other = ex2(o.x - use);
-                    l_all = l * f_own + o.y * f_other;
+                    l_all = l_row * f_own + o.y * f_other;
                     odd_all |= o.z != 0.0f;
                 }
                 if (kBlocks == 1 || active) {
@@ -441,14 +516,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                         if (!live) continue;
                         if (kBf16 && odd_all) {
                             // infinities and NaN among the values of the step's own tokens were taken out of the product
-                            const int64_t from = max(w.a.r.start, int64_t(t0) * kTcTile), to = min(w.a.len, int64_t(t1) * kTcTile);
-                            for (int64_t pos = from; pos < to; ++pos) {
+                            const int from = max(w.a.r.start, t0 * kTcTile), to = min(w.a.r.len, t1 * kTcTile);
+                            for (int pos = from; pos < to; ++pos) {
                                 if (!attend_sees(p, w.a.r.first + tok, tok, pos - w.a.r.start)) continue;
                                 const int page = p.batch.page_table[int64_t(w.b) * p.batch.table_stride + (pos >> p.cache.page_shift)];
                                 if (page < 0 || page >= p.cache.pages) continue;
                                 const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(
                                     p.cache.base[1] + int64_t(page) * p.cache.page_stride + int64_t(w.head) * p.cache.head_stride +
-                                    (pos & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride) + c * 32;
+                                    int64_t(pos & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride) + c * 32;
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) {
                                     const float e = __bfloat162float(v[i]);
@@ -480,151 +555,191 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 ++unit;
                 attend_next_unit(p, w);
             }
+            leave();
+            return;
         } else if (warp < kTcMmaWarp) {
             // ============================================================ producers
-            reg_dec<120>();
+            reg_dec<kTcProducerRegs>();
             const int pt = int(threadIdx.x) - kTcProducerWarp * 32;
             uint32_t bad_any = 0;
             while (true) {
-                const int t0 = w.tile, t1 = int(min(int64_t(w.a.tiles), t0 + (x_end - x0)));
+                const int t0 = w.tile, t1 = min(w.a.tiles, t0 + (x_end - x0));
                 const int tiles = t1 - t0;
                 const int32_t* const table = p.batch.page_table + int64_t(w.b) * p.batch.table_stride;
-                const int64_t len = w.a.len;
+                const int len = w.a.r.len;
                 const int pos_mask = (1 << p.cache.page_shift) - 1;
                 const char* const head_base[2] = {p.cache.base[0] + int64_t(w.head) * p.cache.head_stride,
                                                   p.cache.base[1] + int64_t(w.head) * p.cache.head_stride};
-                auto page_at = [&](int64_t pos) -> int {                     // page number, -1 without one
-                    if (pos >= len) return -1;
+                // Page numbers of four tiles, one group of 16 positions per lane (-1: no page), and the next four on the way.
+                auto load_pages = [&](int n) -> int {
+                    const int pos = (t0 + n) * kTcTile + lane * 16;
+                    if (n + (lane >> 3) >= tiles || pos >= len) return -1;
                     const int page = table[pos >> p.cache.page_shift];
                     return page >= 0 && page < p.cache.pages ? page : -1;
                 };
-                // groups of 16 positions that should have a page and have none
-                auto bad_groups = [&](int64_t pos0) -> uint32_t {
-                    const int64_t pos = pos0 + (lane & 7) * 16;
-                    return __ballot_sync(0xffffffffu, pos < len && page_at(pos) < 0) & 255u;
+                int pages = load_pages(0), pages_next = load_pages(4);
+                int64_t place = 0;                                           // byte offset of the lane's group in the pool
+                auto turn_to = [&](int n) {                                  // tile n (one after the other)
+                    if ((n & 3) != 0) return;
+                    if (n > 0) {
+                        pages = pages_next;
+                        pages_next = load_pages(n + 4);
+                    }
+                    place = pages < 0 ? 0 : int64_t(pages) * p.cache.page_stride + int64_t(((t0 + n) * kTcTile + lane * 16) & pos_mask) * p.cache.token_stride;
+                };
+                auto page_of = [&](int n, int group) { return __shfl_sync(0xffffffffu, pages, (n & 3) * 8 + group); };
+                auto place_of = [&](int n, int group) { return __shfl_sync(0xffffffffu, place, (n & 3) * 8 + group); };
+                // groups of tile n without a page, as far as the sequence reaches
+                auto bad_groups = [&](int n) -> uint32_t {
+                    const bool bad = pages < 0 && (t0 + (n & ~3)) * kTcTile + lane * 16 < len;
+                    return (__ballot_sync(0xffffffffu, bad) >> ((n & 3) * 8)) & 255u;
                 };
                 if (!kBf16) {
                     constexpr int kPieces = kDim / 16;                       // 16-byte pieces of a row of codes
-                    constexpr int kRowsPer = 128 / kPieces;                  // rows one round of the 128 threads covers
+                    constexpr int kRowsPer = kTcProducerThreads / kPieces;   // rows one round of the threads covers
+                    constexpr int kRounds = S::kRounds;
+                    static_assert(kRounds * kRowsPer == kTcTile, "rounds");
+                    char* const raw_gen = smem + S::kOffRaw + pt * 16;
+                    const uint32_t raw_mem = smem_u32(raw_gen);
                     const int piece = pt % kPieces, row0 = pt / kPieces;
-                    uint4 raw[2][kPieces];
-                    float sc[2];
-                    int pages[kPieces], page_own;
-                    auto find = [&](int n) {                                 // pages of tile n
-                        const int64_t pos0 = int64_t(t0 + n) * kTcTile;
-#pragma unroll
-                        for (int i = 0; i < kPieces; ++i) pages[i] = n < tiles ? page_at(pos0 + row0 + i * kRowsPer) : -1;
-                        page_own = n < tiles ? page_at(pos0 + pt) : -1;
-                    };
+                    const uint32_t within = uint32_t(row0 & 15) * uint32_t(p.cache.token_stride) + uint32_t(piece) * 16u;
+                    const int scale_row = pt & 127, scale_of = pt >> 7;      // half of the threads fetch keys' scales, half values'
+                    uint4 last = make_uint4(0, 0, 0, 0);                     // the values' last round
+                    float sc = 0.0f;
+                    bool lack = false;                                       // its row does not exist
+                    // (Whole warp; the tile that `pages` has been turned to.)  Codes wait in shared memory, in slots that only this
+                    // thread uses (a load's destination there takes no line of the first-level cache, which is small beside
+                    // this kernel's shared memory); the last round, for which there is no slot, waits in registers.  Positions
+                    // without a row are filled with zeros.
                     auto fetch = [&](int n, int which) {
-                        const int64_t pos0 = int64_t(t0 + n) * kTcTile;
+                        const int pos0 = (t0 + n) * kTcTile;
 #pragma unroll
-                        for (int i = 0; i < kPieces; ++i) {
-                            const int64_t pos = pos0 + row0 + i * kRowsPer;
-                            raw[which][i] = make_uint4(0, 0, 0, 0);
-                            if (pages[i] >= 0)
-                                raw[which][i] = __ldg(reinterpret_cast<const uint4*>(head_base[which] + int64_t(pages[i]) * p.cache.page_stride +
-                                                                                     (pos & pos_mask) * p.cache.token_stride + piece * 16));
+                        for (int i = 0; i < kRounds; ++i) {
+                            const int row = row0 + i * kRowsPer;
+                            const bool in = page_of(n, row >> 4) >= 0 && pos0 + row < len;
+                            const char* const src = head_base[which] + place_of(n, row >> 4) + (in ? within : 0u);
+                            if (which * kRounds + i < S::kRawSlots) {
+                                cp_async_16(raw_mem + uint32_t(which * kRounds + i) * 4096u, src, in);
+                            } else {
+                                last = __ldg(reinterpret_cast<const uint4*>(src));
+                                lack = !in;
+                            }
                         }
-                        sc[which] = 0.0f;
-                        if (page_own >= 0)
-                            sc[which] = __ldg(p.cache.scale[which] + int64_t(page_own) * p.cache.scale_page_stride + int64_t(w.head) * p.cache.scale_head_stride +
-                                              ((pos0 + pt) & pos_mask));
+                        cp_async_commit();
+                    };
+                    auto fetch_scale = [&](int n) {
+                        const int pos = (t0 + n) * kTcTile + scale_row;
+                        const int page = page_of(n, scale_row >> 4);
+                        const bool in = page >= 0 && pos < len;
+                        sc = __ldg(p.cache.scale[scale_of] + int64_t(in ? page : 0) * p.cache.scale_page_stride + int64_t(w.head) * p.cache.scale_head_stride +
+                                   (in ? pos & pos_mask : 0));
+                        if (!in) sc = 0.0f;
                     };
                     auto store = [&](int which, char* base) {
-                        const int atom = piece / 4;
+                        const int atom = piece / 4, swap = atom & 1, c = (piece & 3) * 2;
+                        // (the two atoms of a row lie on the same banks: their threads store the halves in opposite order)
+                        char* const at0 = base + atom * S::kAtomBytes + row0 * 128 + (((c + swap) ^ (row0 & 7)) << 4);
+                        char* const at1 = base + atom * S::kAtomBytes + row0 * 128 + (((c + 1 - swap) ^ (row0 & 7)) << 4);
 #pragma unroll
-                        for (int i = 0; i < kPieces; ++i) {
-                            const int row = row0 + i * kRowsPer;
+                        for (int i = 0; i < kRounds; ++i) {
+                            uint4 raw;
+                            if (which * kRounds + i < S::kRawSlots) raw = *reinterpret_cast<const uint4*>(raw_gen + (which * kRounds + i) * 4096);
+                            else raw = lack ? make_uint4(0, 0, 0, 0) : last;
                             uint32_t h[8];
-                            codes4_to_f16<kFmt>(raw[which][i].x, h[0], h[1]);
-                            codes4_to_f16<kFmt>(raw[which][i].y, h[2], h[3]);
-                            codes4_to_f16<kFmt>(raw[which][i].z, h[4], h[5]);
-                            codes4_to_f16<kFmt>(raw[which][i].w, h[6], h[7]);
+                            codes4_to_f16<kFmt>(raw.x, h[0], h[1]);
+                            codes4_to_f16<kFmt>(raw.y, h[2], h[3]);
+                            codes4_to_f16<kFmt>(raw.z, h[4], h[5]);
+                            codes4_to_f16<kFmt>(raw.w, h[6], h[7]);
                             const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
-                            char* const at = base + atom * S::kAtomBytes + row * 128;
-                            const int c = (piece & 3) * 2;
-                            // (the two atoms of a row lie on the same banks: their threads store the halves in opposite order)
-                            const int a = atom & 1;
-                            *reinterpret_cast<uint4*>(at + (((c + a) ^ (row & 7)) << 4)) = a ? hi : lo;
-                            *reinterpret_cast<uint4*>(at + (((c + 1 - a) ^ (row & 7)) << 4)) = a ? lo : hi;
+                            *reinterpret_cast<uint4*>(at0 + i * kRowsPer * 128) = swap ? hi : lo;      // (kRowsPer: a multiple of 8)
+                            *reinterpret_cast<uint4*>(at1 + i * kRowsPer * 128) = swap ? lo : hi;
                         }
                     };
-                    find(0);
-                    fetch(0, 0);
-                    fetch(0, 1);
-                    for (int n = 0; n < tiles; ++n) {
+                    // one round ahead: tile n + 1 is asked for while tile n is stored
+#pragma unroll 1
+                    for (int n = -1; n < tiles; ++n) {
                         const uint32_t at = tiles_before + n;
-                        const uint32_t ki = uint32_t(at % S::kKStages), vi = uint32_t(at % S::kVStages);
-                        const uint32_t bad = bad_groups(int64_t(t0 + n) * kTcTile);
-                        const float ks = sc[0], vs = sc[1];
-                        find(n + 1);
-                        alive = warp_wait(&bars.k_empty[ki], (uint32_t(at / S::kKStages) & 1u) ^ 1u);
-                        if (!alive) break;
-                        store(0, smem + S::kOffK + ki * S::kOperand);
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&bars.k_full[ki]);
-                        if (n + 1 < tiles) fetch(n + 1, 0);
-                        alive = warp_wait(&bars.v_empty[vi], (uint32_t(at / S::kVStages) & 1u) ^ 1u);
-                        if (!alive) break;
-                        store(1, smem + S::kOffV + vi * S::kOperand);
-                        {
-                            float* const to = scales + vi * 3 * kTcTile + pt;
-                            const float v = vs >= 1e-30f ? vs : 1e-30f;          // a row of zero values keeps its weight in the sum
-                            to[0] = ks;
-                            to[kTcTile] = fmaf(vs, 0.0f, lg2(v));                // a NaN scale reaches the score alone
-                            to[2 * kTcTile] = __fdividef(1.0f, v);
+                        const uint32_t ki = at % S::kKStages, vi = at % S::kVStages;
+                        const bool more = n + 1 < tiles;
+                        float s_now = sc;
+                        uint32_t bad = 0;
+                        if (n >= 0) {
+                            bad = bad_groups(n);
+                            alive = warp_wait(&bars.k_empty[ki], ((at / S::kKStages) & 1u) ^ 1u);
+                            if (!alive) break;
+                            cp_async_wait<1>();                              // (the keys were asked for before the values)
+                            store(0, smem + S::kOffK + ki * S::kOperand);
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&bars.k_full[ki]);
                         }
-                        if (pt == 0) bars.meta[vi] = bad;
-                        bad_any |= bad;
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&bars.v_full[vi]);
-                        if (n + 1 < tiles) fetch(n + 1, 1);
+                        if (more) {
+                            turn_to(n + 1);
+                            fetch(n + 1, 0);
+                            fetch_scale(n + 1);
+                        } else {
+                            cp_async_commit();
+                        }
+                        if (n >= 0) {
+                            alive = warp_wait(&bars.v_empty[vi], ((at / S::kVStages) & 1u) ^ 1u);
+                            if (!alive) break;
+                            cp_async_wait<1>();
+                            store(1, smem + S::kOffV + vi * S::kOperand);
+                            float* const to = scales + vi * 3 * kTcTile + scale_row;
+                            if (scale_of == 0) {
+                                to[0] = s_now;
+                            } else {
+                                const float v = s_now >= 1e-30f ? s_now : 1e-30f;    // a row of zero values keeps its weight in the sum
+                                to[kTcTile] = fmaf(s_now, 0.0f, lg2(v));             // a NaN scale reaches the score alone
+                                to[2 * kTcTile] = __fdividef(1.0f, v);
+                            }
+                            if (pt == 0) bars.meta[vi] = bad;
+                            bad_any |= bad;
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&bars.v_full[vi]);
+                        }
+                        if (more) fetch(n + 1, 1);
                     }
                 } else {
+#pragma unroll 1
                     for (int n = 0; n < tiles; ++n) {
                         const uint32_t at = tiles_before + n;
-                        const int64_t pos0 = int64_t(t0 + n) * kTcTile;
-                        const uint32_t stage[2] = {uint32_t(at % S::kKStages), uint32_t(at % S::kVStages)};
-                        const uint32_t phase[2] = {(uint32_t(at / S::kKStages) & 1u) ^ 1u, (uint32_t(at / S::kVStages) & 1u) ^ 1u};
-                        const uint32_t bad = bad_groups(pos0);
+                        const int pos0 = (t0 + n) * kTcTile;
+                        const uint32_t ki = at % S::kKStages, vi = at % S::kVStages;
+                        turn_to(n);
+                        const uint32_t bad = bad_groups(n);
                         bad_any |= bad;
                         const bool plain = bad == 0 && pos0 + kTcTile <= w.a.r.start;     // whole, and the context's alone
-#pragma unroll
+#pragma unroll 1
                         for (int which = 0; which < 2; ++which) {
-                            uint64_t* const full = which ? &bars.v_full[stage[1]] : &bars.k_full[stage[0]];
-                            char* const dst = smem + (which ? S::kOffV : S::kOffK) + stage[which] * S::kOperand;
-                            alive = alive && warp_wait(which ? &bars.v_empty[stage[1]] : &bars.k_empty[stage[0]], phase[which]);
+                            uint64_t* const full = which ? &bars.v_full[vi] : &bars.k_full[ki];
+                            char* const dst = smem + (which ? S::kOffV + vi * S::kOperand : S::kOffK + ki * S::kOperand);
+                            alive = which ? warp_wait(&bars.v_empty[vi], ((at / S::kVStages) & 1u) ^ 1u)
+                                          : warp_wait(&bars.k_empty[ki], ((at / S::kKStages) & 1u) ^ 1u);
                             if (!alive) break;
+                            bool odd = false;
                             if (plain) {
-                                if (which && pt == 0) bars.meta[stage[1]] = 0;
-                                if (which && lane == 0) bars.odd[stage[1]][warp - kTcProducerWarp] = 0;
+                                // one box per lane, spread over the warps: an instruction holds its thread for some 100 clocks
                                 if (pt == 0) {
+                                    if (which) bars.meta[vi] = 0, bars.odd[vi][0] = 0;   // (ahead of this thread's arrival)
                                     mbar_arrive_expect_tx(full, S::kOperand);
-                                    for (int t = 0; t < kTcTile; t += tp.box_tokens) {
-                                        const int64_t pos = pos0 + t;
-                                        const int page = page_at(pos);
-                                        for (int a = 0; a < S::kAtoms; ++a)
-                                            tma_load_4d(smem_u32(dst + a * S::kAtomBytes + t * 128), &tp.map[which], full, a * 64,
-                                                        int(pos & pos_mask), w.head, page);
-                                    }
-                                } else if (lane == 0) {
-                                    mbar_arrive(full);
                                 }
+                                const int k = lane * kTcProducers + warp - kTcProducerWarp;
+                                const int t = k / S::kAtoms * 16, a = k % S::kAtoms;
+                                const int page = page_of(n, (t >> 4) & 7);
+                                if (t < kTcTile && (t & (tp.box_tokens - 1)) == 0)
+                                    tma_load_4d(smem_u32(dst + a * S::kAtomBytes + t * 128), &tp.map[which], full, a * 64, (pos0 + t) & pos_mask, w.head, page);
                             } else {
-                                bool odd = false;
                                 constexpr int kPieces = kDim / 8;
                                 const int piece = pt % kPieces;
 #pragma unroll 4
-                                for (int row = pt / kPieces; row < kTcTile; row += 128 / kPieces) {
-                                    const int64_t pos = pos0 + row;
-                                    const int page = page_at(pos);
-                                    uint4 v = make_uint4(0, 0, 0, 0);
-                                    if (page >= 0)
-                                        v = __ldg(reinterpret_cast<const uint4*>(head_base[which] + int64_t(page) * p.cache.page_stride +
-                                                                                 (pos & pos_mask) * p.cache.token_stride + piece * 16));
+                                for (int row = pt / kPieces; row < kTcTile; row += kTcProducerThreads / kPieces) {
+                                    const int pos = pos0 + row;
+                                    const bool in = page_of(n, row >> 4) >= 0 && pos < len;
+                                    const int64_t off = place_of(n, row >> 4) + (in ? uint32_t(row & 15) * uint32_t(p.cache.token_stride) : 0u);
+                                    uint4 v = __ldg(reinterpret_cast<const uint4*>(head_base[which] + off + piece * 16));
+                                    if (!in) v = make_uint4(0, 0, 0, 0);
                                     if (which && pos >= w.a.r.start) {
                                         // values of the step's own tokens: rows differ in what they see, so what is not finite
                                         // stays out of the product (a weight of 0 would not keep it out)
@@ -638,18 +753,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                                     }
                                     *reinterpret_cast<uint4*>(dst + (piece / 8) * S::kAtomBytes + row * 128 + (((piece % 8) ^ (row & 7)) << 4)) = v;
                                 }
-                                const bool any_odd = __any_sync(0xffffffffu, odd) != 0;
-                                if (which && pt == 0) bars.meta[stage[1]] = bad;
-                                if (which && lane == 0) bars.odd[stage[1]][warp - kTcProducerWarp] = any_odd;
                                 fence_proxy_async_smem();
-                                __syncwarp();
-                                if (lane == 0) mbar_arrive(full);
                             }
+                            const bool any_odd = __any_sync(0xffffffffu, odd) != 0;
+                            if (which && pt == 0 && !plain) bars.meta[vi] = bad;
+                            if (which && lane == 0 && !(plain && pt == 0)) bars.odd[vi][warp - kTcProducerWarp] = any_odd;
+                            __syncwarp();
+                            if (lane == 0 && !(plain && pt == 0)) mbar_arrive(full);
                         }
                         if (!alive) break;
                     }
                 }
-                if (w.a.r.cut) bad_any |= 1u;
+                if (w.a.r.n > w.a.r.len - w.a.r.start) bad_any |= 1u;
                 if (!alive) break;
                 x0 += tiles;
                 if (x0 >= x_end) break;
@@ -657,38 +772,48 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 attend_next_unit(p, w);
             }
             if (bad_any && pt == 0) atomicCAS(p.status, 0u, kBadPage);
+            if (kBf16 && !alive) {                             // gave up: wait (with a limit) for the copies in flight
+                const uint64_t since = global_timer_ns();
+                while (global_timer_ns() - since < 2000000ull) {}
+            }
+            leave();
+            return;
         } else {
             // ============================================================ matrix instructions
-            reg_dec<56>();
+            reg_dec<kTcMmaRegs>();
             if (warp == kTcMmaWarp && lane == 0) {
-            const uint32_t kind = kBf16 ? (1u << 7) | (1u << 10) : 0u;
-            const uint32_t idesc_s = (1u << 4) | kind | ((128u >> 3) << 17) | ((128u >> 4) << 24);
-            const uint32_t idesc_o = (1u << 4) | kind | (1u << 16) | ((uint32_t(kDim) >> 3) << 17) | ((128u >> 4) << 24);
-            const uint64_t k_hi = tc_desc_hi(16u, 1024u), v_hi = tc_desc_hi(uint32_t(S::kAtomBytes), 1024u);
-            const uint32_t q_addr = smem_u32(smem), k_addr = smem_u32(smem + S::kOffK), v_addr = smem_u32(smem + S::kOffV);
+            constexpr uint32_t kind = kBf16 ? (1u << 7) | (1u << 10) : 0u;
+            constexpr uint32_t idesc_s = (1u << 4) | kind | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+            constexpr uint32_t idesc_o = (1u << 4) | kind | (1u << 16) | ((uint32_t(kDim) >> 3) << 17) | ((128u >> 4) << 24);
+            // Operand descriptors in halves: the issuing thread is alone in its warp and every instruction between two
+            // products costs it several clocks, so a step adds a constant to a word that is otherwise ready.
+            // (128-byte swizzle, descriptor version 1; 8-row groups 1024 bytes apart; V's 64-column atoms kAtomBytes apart)
+            constexpr uint32_t kHi = (1024u >> 4) | 1u << 14 | 2u << 29;
+            constexpr uint32_t kStep = uint32_t(S::kOperand) >> 4;
+            const uint32_t q_lo = (smem_u32(smem) >> 4) | 1u << 16, k_lo = (smem_u32(smem + S::kOffK) >> 4) | 1u << 16;
+            const uint32_t v_lo = (smem_u32(smem + S::kOffV) >> 4) | uint32_t(S::kAtomBytes >> 4) << 16;
             uint32_t p_phase = 0;                            // bit x: parity of stream x's next product
-            auto desc = [](uint32_t addr, uint64_t hi) { return uint64_t((addr & 0x3FFFFu) >> 4) | hi; };
             auto scores = [&](int x, uint32_t stage) {
-                const uint32_t q = q_addr + (kBlocks == 2 ? uint32_t(x) * S::kOperand : 0u), k = k_addr + stage * S::kOperand;
+                const uint32_t q = q_lo + (kBlocks == 2 ? uint32_t(x) * kStep : 0u), k = k_lo + stage * kStep, to = tmem + S::kS + uint32_t(x) * 128u;
 #pragma unroll
                 for (int j = 0; j < kDim / 16; ++j) {
-                    const uint32_t off = uint32_t(j >> 2) * S::kAtomBytes + uint32_t(j & 3) * 32u;
-                    umma_bf16(tmem + S::kS + uint32_t(x) * 128u, desc(q + off, k_hi), desc(k + off, k_hi), idesc_s, j > 0);
+                    constexpr uint32_t kAtom = uint32_t(S::kAtomBytes) >> 4;
+                    const uint32_t off = uint32_t(j >> 2) * kAtom + uint32_t(j & 3) * 2u;
+                    umma_split<false>(to, q + off, kHi, k + off, kHi, idesc_s, j > 0);
                 }
                 umma_commit(&bars.s_full[x]);
             };
-            auto values = [&](int x, uint32_t stage, bool first) {
-                const uint32_t v = v_addr + stage * S::kOperand;
+            auto values = [&](int x, uint32_t stage, uint32_t go_on) {
+                const uint32_t v = v_lo + stage * kStep, to = tmem + S::kO + uint32_t(x) * 128u, from = tmem + S::kS + uint32_t(x) * 128u;
 #pragma unroll
                 for (int j = 0; j < kTcTile / 16; ++j)
-                    umma_ts(tmem + S::kO + uint32_t(x) * 128u, tmem + S::kS + uint32_t(x) * 128u + uint32_t(j) * 8u,
-                            desc(v + uint32_t(j) * 2048u, v_hi), idesc_o, j > 0 || !first);
+                    umma_ts(to, from + uint32_t(j) * 8u, v + uint32_t(j) * (2048u >> 4), kHi, idesc_o, j > 0 ? 1u : go_on);
                 umma_commit(&bars.pv_done[x]);
             };
             auto k_wait = [&](uint32_t at) { return wait(&bars.k_full[at % S::kKStages], uint32_t(at / S::kKStages) & 1u); };
             auto v_wait = [&](uint32_t at) { return wait(&bars.v_full[at % S::kVStages], uint32_t(at / S::kVStages) & 1u); };
             while (true) {
-                const int t0 = w.tile, t1 = int(min(int64_t(w.a.tiles), t0 + (x_end - x0)));
+                const int t0 = w.tile, t1 = min(w.a.tiles, t0 + (x_end - x0));
                 const int tiles = t1 - t0;
                 const int unit_rows = min(S::kRows, w.a.r.n * p.group - w.block * S::kRows);
                 const int streams = kBlocks == 2 ? (unit_rows > 128 ? 2 : 1) : min(tiles, 2);
@@ -711,7 +836,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                         alive = v_wait(at) && wait(&bars.p_full[x], p_phase >> x & 1u);
                         if (!alive) break;
                         tc_fence_after_sync();
-                        values(x, vi, n < (kBlocks == 2 ? 1 : 2));
+                        values(x, vi, n >= (kBlocks == 2 ? 1 : 2));
                         if (kBlocks == 1 || x == streams - 1) umma_commit(&bars.v_empty[vi]);
                         const int next = n + (kBlocks == 2 ? 1 : 2);
                         if (next < tiles) {
@@ -738,18 +863,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
             const uint64_t since = global_timer_ns();
             while (!mbar_try_wait(&bars.drained, 0) && global_timer_ns() - since < 2 * tp.wait_ns) {}
             }
-        }
-        // a producer that gave up waits (with a limit) for its own copies in flight
-        if (kBf16 && !alive && warp == kTcProducerWarp && lane == 0) {
-            const uint64_t since = global_timer_ns();
-            while (global_timer_ns() - since < 2000000ull) {}
+            leave();
+            return;
         }
     }
-    __syncwarp();
-    tc_fence_before_sync();
-    __syncthreads();
-    tc_fence_after_sync();
-    if (warp == kTcMmaWarp) tmem_dealloc(tmem, 512);
+    leave();
 }
 
 #endif  // __CUDACC__

@@ -31,6 +31,8 @@ struct KvBatchView {
     int requests, tokens;
 };
 
+constexpr int64_t kKvMaxTokens = int64_t(1) << 30;         // of one sequence
+
 // Checks a cache / batch description and turns it into the view (host).
 int kv_view(const tl_kv_cache* c, KvView* out);
 int kv_batch_view(const tl_kv_batch* b, KvBatchView* out);
@@ -43,20 +45,23 @@ inline int kv_item(int format) { return format == TL_KV_BF16 ? 2 : 1; }
 // inside what the page table can address.
 struct KvRequest {
     int first, n;               // its rows
-    int64_t start;              // tokens in the cache before the step's
-    bool cut;                   // its tokens did not fit the page table
+    int start;                  // tokens in the cache before the step's
+    int len;                    // positions that exist: start + n, as far as the page table reaches
 };
+// Positions the page table of a request can address (at most 2^30: a position fits 32 bits with room to spare).
+__device__ __forceinline__ int kv_room(const KvBatchView& bv, int page_shift) {
+    return int(min(bv.table_stride << page_shift, int64_t(1) << 30));
+}
 __device__ __forceinline__ KvRequest kv_request(const KvBatchView& bv, int page_shift, int b) {
     KvRequest r;
     int a = bv.offsets[b], e = bv.offsets[b + 1];
     a = min(max(a, 0), bv.tokens);
     e = min(max(e, a), bv.tokens);
-    const int64_t room = bv.table_stride << page_shift;
-    const int64_t s = max(bv.start[b], 0);
+    const int room = kv_room(bv, page_shift);
     r.first = a;
     r.n = e - a;
-    r.start = s < room ? s : room;
-    r.cut = s + r.n > room;
+    r.start = min(max(bv.start[b], 0), room);
+    r.len = r.n < room - r.start ? r.start + r.n : room;
     return r;
 }
 

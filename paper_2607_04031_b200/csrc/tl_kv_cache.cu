@@ -91,13 +91,12 @@ __device__ __forceinline__ int warp_request_of(const KvBatchView& bv, int row) {
 }
 
 // Address of a position's row in the cache (keys or values), or null when there is no page for it.
-__device__ __forceinline__ char* kv_row(const KvView& c, const KvBatchView& bv, int b, int64_t pos, int which, int head,
+__device__ __forceinline__ char* kv_row(const KvView& c, const KvBatchView& bv, int b, int pos, int which, int head,
                                         float** scale) {
-    const int64_t slot = pos >> c.page_shift;
-    if (slot < 0 || slot >= bv.table_stride) return nullptr;
-    const int64_t page = bv.page_table[int64_t(b) * bv.table_stride + slot];
+    if (pos < 0 || pos >= kv_room(bv, c.page_shift)) return nullptr;
+    const int64_t page = bv.page_table[int64_t(b) * bv.table_stride + (pos >> c.page_shift)];
     if (page < 0 || page >= c.pages) return nullptr;
-    const int64_t line = pos & ((int64_t(1) << c.page_shift) - 1);
+    const int line = pos & ((1 << c.page_shift) - 1);
     if (scale) *scale = c.scale[which] + page * c.scale_page_stride + int64_t(head) * c.scale_head_stride + line;
     return c.base[which] + page * c.page_stride + int64_t(head) * c.head_stride + line * c.token_stride;
 }
