@@ -6,12 +6,14 @@
 
 namespace tl {
 
-// Joins the units that cross a border between CTA ranges.  Block c looks at the border in front of CTA c + 1; the
-// borders inside one unit share its rows out among themselves.
-constexpr int kCombineThreads = 256;
+// Joins the units that cross a border between CTA ranges.  Blocks (c, *) look at the border in front of CTA c + 1; the
+// borders inside one unit share its rows out among themselves, and so do the blocks of a border (one per 16 rows of the
+// unit: with one block a border, 256-row units took 33 to 60 us here, a chain of dependent loads per row).
+constexpr int kCombineThreads = 256, kCombineRows = 16;
 __global__ void __launch_bounds__(kCombineThreads) attend_combine_kernel(const AttendParams p, int dim) {
-    pdl_wait();
     pdl_launch_dependents();
+    // (The lengths may be read ahead of the wait: every CTA of the attention kernel has let this one start after its own
+    // wait, so whatever wrote them is over.)
     const int total = attend_total(p), per = attend_per_cta(total, p.ctas);
     const int64_t border64 = (int64_t(blockIdx.x) + 1) * per;
     if (border64 >= total) return;
@@ -20,9 +22,10 @@ __global__ void __launch_bounds__(kCombineThreads) attend_combine_kernel(const A
     if (w.tile == 0) return;                                  // the border lies between two units
     const int u0 = border - w.tile, u1 = u0 + w.a.tiles;
     const int c0 = int(uint32_t(u0) / uint32_t(per)), c1 = int(uint32_t(u1 - 1) / uint32_t(per));
-    const int share = int(blockIdx.x) - c0, shares = c1 - c0;
+    const int share = (int(blockIdx.x) - c0) * int(gridDim.y) + int(blockIdx.y), shares = (c1 - c0) * int(gridDim.y);
     const int rows = min(p.rows_block, w.a.r.n * p.group - w.block * p.rows_block);
     const int vecs = dim / 4;
+    pdl_wait();
     for (int e = share * kCombineThreads + threadIdx.x; e < rows * vecs; e += shares * kCombineThreads) {
         const int r = e / vecs, d = e % vecs * 4;
         // CTA c0 ends inside the unit it began (its second slot); the others begin inside it (their first)
@@ -156,7 +159,7 @@ int tl_tree_attention(const tl_kv_cache* cache, const tl_kv_batch* batch, const 
         return rc;
     if (plan.part_bytes == 0) return TL_OK;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(plan.ctas - 1));
+    cfg.gridDim = dim3(unsigned(plan.ctas - 1), unsigned(plan.mma_rows / kCombineRows));
     cfg.blockDim = dim3(kCombineThreads);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];

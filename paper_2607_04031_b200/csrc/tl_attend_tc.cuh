@@ -606,6 +606,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     const int scale_row = pt & 127, scale_of = pt >> 7;      // half of the threads fetch keys' scales, half values'
                     uint4 last = make_uint4(0, 0, 0, 0);                     // the values' last round
                     float sc = 0.0f;
+                    bool sc_lack = false;
                     bool lack = false;                                       // its row does not exist
                     // (Whole warp; the tile that `pages` has been turned to.)  Codes wait in shared memory, in slots that only this
                     // thread uses (a load's destination there takes no line of the first-level cache, which is small beside
@@ -633,7 +634,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                         const bool in = page >= 0 && pos < len;
                         sc = __ldg(p.cache.scale[scale_of] + int64_t(in ? page : 0) * p.cache.scale_page_stride + int64_t(w.head) * p.cache.scale_head_stride +
                                    (in ? pos & pos_mask : 0));
-                        if (!in) sc = 0.0f;
+                        sc_lack = !in;                                       // (zeroed at its use: here it would be waited for)
                     };
                     auto store = [&](int which, char* base) {
                         const int atom = piece / 4, swap = atom & 1, c = (piece & 3) * 2;
@@ -661,7 +662,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                         const uint32_t at = tiles_before + n;
                         const uint32_t ki = at % S::kKStages, vi = at % S::kVStages;
                         const bool more = n + 1 < tiles;
-                        float s_now = sc;
+                        const float s_raw = sc;
+                        const bool s_lack = sc_lack;
                         uint32_t bad = 0;
                         if (n >= 0) {
                             bad = bad_groups(n);
@@ -686,6 +688,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             cp_async_wait<1>();
                             store(1, smem + S::kOffV + vi * S::kOperand);
                             float* const to = scales + vi * 3 * kTcTile + scale_row;
+                            const float s_now = s_lack ? 0.0f : s_raw;
                             if (scale_of == 0) {
                                 to[0] = s_now;
                             } else {
