@@ -90,19 +90,18 @@ attend_kernel(const AttendParams p) {
         const int pos_first = t0 * S::kTile + warp * 16;
         int count = t1 - t0;
         if (pos_first + (count - 1) * S::kTile >= len) --count;          // only the unit's last tile can begin past the end
-        auto page_of = [&](int i) -> int {                               // page number, or -1
-            if (i >= count) return -1;
-            const int page = table[(pos_first + i * S::kTile) >> p.cache.page_shift];   // (slot is inside the table: pos < len)
-            return page >= 0 && page < p.cache.pages ? page : -1;
-        };
-        // page numbers of 32 sub-tiles, one per lane, the next 32 on the way
-        int pages = page_of(lane), pages_next = page_of(lane + 32);
+        // Page numbers of 32 sub-tiles, one per lane, and the next 32 on the way (checked when their turn comes: where they
+        // are asked for they would be waited for).
+        auto load_page = [&](int i) -> int { return __ldg(table + (i < count ? (pos_first + i * S::kTile) >> p.cache.page_shift : 0)); };
+        auto checked = [&](int page, int i) { return i < count && page >= 0 && page < p.cache.pages ? page : -1; };
+        int pages = load_page(lane), pages_next = load_page(lane + 32);
+        pages = checked(pages, lane);
         uint32_t bad_any = 0;
         auto issue = [&](int i) {                                        // starts the copies of sub-tile i (whole warp, i upwards)
             if (i < count) {
                 if (i > 0 && (i & 31) == 0) {
-                    pages = pages_next;
-                    pages_next = page_of(i + 32 + lane);
+                    pages = checked(pages_next, i + lane);
+                    pages_next = load_page(i + 32 + lane);
                 }
                 const int page = __shfl_sync(0xffffffffu, pages, i & 31);
                 const bool ok = page >= 0;

@@ -571,20 +571,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 const char* const head_base[2] = {p.cache.base[0] + int64_t(w.head) * p.cache.head_stride,
                                                   p.cache.base[1] + int64_t(w.head) * p.cache.head_stride};
                 // Page numbers of four tiles, one group of 16 positions per lane (-1: no page), and the next four on the way.
-                auto load_pages = [&](int n) -> int {
-                    const int pos = (t0 + n) * kTcTile + lane * 16;
-                    if (n + (lane >> 3) >= tiles || pos >= len) return -1;
-                    const int page = table[pos >> p.cache.page_shift];
-                    return page >= 0 && page < p.cache.pages ? page : -1;
-                };
-                int pages = load_pages(0), pages_next = load_pages(4);
+                // (Entries are checked when their turn comes: here they would be waited for.)
+                auto there = [&](int n) { return n + (lane >> 3) < tiles && (t0 + n) * kTcTile + lane * 16 < len; };
+                auto load_pages = [&](int n) -> int { return __ldg(table + (there(n) ? ((t0 + n) * kTcTile + lane * 16) >> p.cache.page_shift : 0)); };
+                int pages = 0, pages_next = load_pages(0);
                 int64_t place = 0;                                           // byte offset of the lane's group in the pool
                 auto turn_to = [&](int n) {                                  // tile n (one after the other)
                     if ((n & 3) != 0) return;
-                    if (n > 0) {
-                        pages = pages_next;
-                        pages_next = load_pages(n + 4);
-                    }
+                    pages = there(n) && pages_next >= 0 && pages_next < p.cache.pages ? pages_next : -1;
+                    pages_next = load_pages(n + 4);
                     place = pages < 0 ? 0 : int64_t(pages) * p.cache.page_stride + int64_t(((t0 + n) * kTcTile + lane * 16) & pos_mask) * p.cache.token_stride;
                 };
                 auto page_of = [&](int n, int group) { return __shfl_sync(0xffffffffu, pages, (n & 3) * 8 + group); };
