@@ -657,8 +657,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                         const uint32_t at = tiles_before + n;
                         const uint32_t ki = at % S::kKStages, vi = at % S::kVStages;
                         const bool more = n + 1 < tiles;
-                        const float s_raw = sc;
-                        const bool s_lack = sc_lack;
                         uint32_t bad = 0;
                         if (n >= 0) {
                             bad = bad_groups(n);
@@ -673,7 +671,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                         if (more) {
                             turn_to(n + 1);
                             fetch(n + 1, 0);
-                            fetch_scale(n + 1);
                         } else {
                             cp_async_commit();
                         }
@@ -683,7 +680,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             cp_async_wait<1>();
                             store(1, smem + S::kOffV + vi * S::kOperand);
                             float* const to = scales + vi * 3 * kTcTile + scale_row;
-                            const float s_now = s_lack ? 0.0f : s_raw;
+                            const float s_now = sc_lack ? 0.0f : sc;
                             if (scale_of == 0) {
                                 to[0] = s_now;
                             } else {
@@ -697,7 +694,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             __syncwarp();
                             if (lane == 0) mbar_arrive(&bars.v_full[vi]);
                         }
-                        if (more) fetch(n + 1, 1);
+                        if (more) {
+                            fetch(n + 1, 1);
+                            fetch_scale(n + 1);                              // (behind the use of the last one: a copy of it would be waited for)
+                        }
                     }
                 } else {
 #pragma unroll 1
