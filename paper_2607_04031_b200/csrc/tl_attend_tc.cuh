@@ -580,7 +580,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     if ((n & 3) != 0) return;
                     pages = there(n) && pages_next >= 0 && pages_next < p.cache.pages ? pages_next : -1;
                     pages_next = load_pages(n + 4);
-                    place = pages < 0 ? 0 : int64_t(pages) * p.cache.page_stride + int64_t(((t0 + n) * kTcTile + lane * 16) & pos_mask) * p.cache.token_stride;
+                    place = pages < 0 ? -1 : int64_t(pages) * p.cache.page_stride + int64_t(((t0 + n) * kTcTile + lane * 16) & pos_mask) * p.cache.token_stride;
                 };
                 auto page_of = [&](int n, int group) { return __shfl_sync(0xffffffffu, pages, (n & 3) * 8 + group); };
                 auto place_of = [&](int n, int group) { return __shfl_sync(0xffffffffu, place, (n & 3) * 8 + group); };
@@ -596,7 +596,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     static_assert(kRounds * kRowsPer == kTcTile, "rounds");
                     char* const raw_gen = smem + S::kOffRaw + pt * 16;
                     const uint32_t raw_mem = smem_u32(raw_gen);
-                    const int piece = pt % kPieces, row0 = pt / kPieces;
+                    // Eight neighbouring lanes cover four pieces of two rows: their stores of the swizzled halves fall on
+                    // different banks (the two 64-dimension atoms of a row lie on the same ones).
+                    const int piece = kPieces == 8 ? (lane & 3) | (lane >> 4) << 2 : lane & 3;
+                    const int row0 = kPieces == 8 ? (pt >> 5) * 4 + ((lane >> 2) & 3) : pt >> 2;
                     const uint32_t within = uint32_t(row0 & 15) * uint32_t(p.cache.token_stride) + uint32_t(piece) * 16u;
                     const int scale_row = pt & 127, scale_of = pt >> 7;      // half of the threads fetch keys' scales, half values'
                     uint4 last = make_uint4(0, 0, 0, 0);                     // the values' last round
@@ -607,13 +610,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     // thread uses (a load's destination there takes no line of the first-level cache, which is small beside
                     // this kernel's shared memory); the last round, for which there is no slot, waits in registers.  Positions
                     // without a row are filled with zeros.
-                    auto fetch = [&](int n, int which) {
+                    int64_t from[kRounds];                                   // of tile n + 1: byte offset in the pool, -1 without a row
+                    auto locate = [&](int n) {
                         const int pos0 = (t0 + n) * kTcTile;
 #pragma unroll
                         for (int i = 0; i < kRounds; ++i) {
                             const int row = row0 + i * kRowsPer;
-                            const bool in = page_of(n, row >> 4) >= 0 && pos0 + row < len;
-                            const char* const src = head_base[which] + place_of(n, row >> 4) + (in ? within : 0u);
+                            const int64_t at = place_of(n, row >> 4);
+                            from[i] = at >= 0 && pos0 + row < len ? at + within : -1;
+                        }
+                    };
+                    auto fetch = [&](int which) {
+#pragma unroll
+                        for (int i = 0; i < kRounds; ++i) {
+                            const bool in = from[i] >= 0;
+                            const char* const src = head_base[which] + (in ? from[i] : 0);
                             if (which * kRounds + i < S::kRawSlots) {
                                 cp_async_16(raw_mem + uint32_t(which * kRounds + i) * 4096u, src, in);
                             } else {
@@ -632,10 +643,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                         sc_lack = !in;                                       // (zeroed at its use: here it would be waited for)
                     };
                     auto store = [&](int which, char* base) {
-                        const int atom = piece / 4, swap = atom & 1, c = (piece & 3) * 2;
-                        // (the two atoms of a row lie on the same banks: their threads store the halves in opposite order)
-                        char* const at0 = base + atom * S::kAtomBytes + row0 * 128 + (((c + swap) ^ (row0 & 7)) << 4);
-                        char* const at1 = base + atom * S::kAtomBytes + row0 * 128 + (((c + 1 - swap) ^ (row0 & 7)) << 4);
+                        const int c = (piece & 3) * 2;
+                        char* const at0 = base + (piece >> 2) * S::kAtomBytes + row0 * 128 + ((c ^ (row0 & 7)) << 4);
+                        char* const at1 = base + (piece >> 2) * S::kAtomBytes + row0 * 128 + (((c + 1) ^ (row0 & 7)) << 4);
 #pragma unroll
                         for (int i = 0; i < kRounds; ++i) {
                             uint4 raw;
@@ -646,9 +656,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             codes4_to_f16<kFmt>(raw.y, h[2], h[3]);
                             codes4_to_f16<kFmt>(raw.z, h[4], h[5]);
                             codes4_to_f16<kFmt>(raw.w, h[6], h[7]);
-                            const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
-                            *reinterpret_cast<uint4*>(at0 + i * kRowsPer * 128) = swap ? hi : lo;      // (kRowsPer: a multiple of 8)
-                            *reinterpret_cast<uint4*>(at1 + i * kRowsPer * 128) = swap ? lo : hi;
+                            *reinterpret_cast<uint4*>(at0 + i * kRowsPer * 128) = make_uint4(h[0], h[1], h[2], h[3]);      // (kRowsPer: a multiple of 8)
+                            *reinterpret_cast<uint4*>(at1 + i * kRowsPer * 128) = make_uint4(h[4], h[5], h[6], h[7]);
                         }
                     };
                     // one round ahead: tile n + 1 is asked for while tile n is stored
@@ -670,7 +679,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                         }
                         if (more) {
                             turn_to(n + 1);
-                            fetch(n + 1, 0);
+                            locate(n + 1);
+                            fetch(0);
                         } else {
                             cp_async_commit();
                         }
@@ -695,7 +705,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             if (lane == 0) mbar_arrive(&bars.v_full[vi]);
                         }
                         if (more) {
-                            fetch(n + 1, 1);
+                            fetch(1);
                             fetch_scale(n + 1);                              // (behind the use of the last one: a copy of it would be waited for)
                         }
                     }
@@ -734,8 +744,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
 #pragma unroll 4
                                 for (int row = pt / kPieces; row < kTcTile; row += kTcProducerThreads / kPieces) {
                                     const int pos = pos0 + row;
-                                    const bool in = page_of(n, row >> 4) >= 0 && pos < len;
-                                    const int64_t off = place_of(n, row >> 4) + (in ? uint32_t(row & 15) * uint32_t(p.cache.token_stride) : 0u);
+                                    const int64_t at = place_of(n, row >> 4);
+                                    const bool in = at >= 0 && pos < len;
+                                    const int64_t off = in ? at + uint32_t(row & 15) * uint32_t(p.cache.token_stride) : 0;
                                     uint4 v = __ldg(reinterpret_cast<const uint4*>(head_base[which] + off + piece * 16));
                                     if (!in) v = make_uint4(0, 0, 0, 0);
                                     if (which && pos >= w.a.r.start) {
