@@ -480,9 +480,8 @@ def _cuda(t: torch.Tensor, name: str, dtype=None, dims=None) -> torch.Tensor:
 
 
 def _int32(t: torch.Tensor, name: str, shape) -> int:
-    _cuda(t, name, torch.int32)
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype is not torch.int32 or not t.is_cuda or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous CUDA tensor of int32 and shape {tuple(shape)}, got {t.dtype}, {tuple(t.shape)}")
     return t.data_ptr()
 
 
@@ -510,7 +509,7 @@ def kv_cache(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = No
         c.scale_page_stride, c.scale_head_stride = k_scale.stride()[:2]
     elif k_scale is not None or v_scale is not None:
         raise ValueError("a bf16 cache has no scales")
-    c._tensors, c._ref = (k, v, k_scale, v_scale), ctypes.byref(c)
+    c._tensors, c._ref, c._device = (k, v, k_scale, v_scale), ctypes.byref(c), k.device.index
     return c
 
 
@@ -528,45 +527,55 @@ def kv_batch(page_table: torch.Tensor, start: torch.Tensor, token_offsets: torch
     return b
 
 
-def _kv_rows(t: torch.Tensor, name: str, cache: KvCache, batch: KvBatch):
-    """(pointer, row stride, element type) of a step's [tokens, heads, head_dim] tensor."""
-    _cuda(t, name, dims=3)
-    if t.dtype not in _ELEMS:
-        raise ValueError(f"{name}: expected bf16 or fp32, got {t.dtype}")
-    if tuple(t.shape) != (batch.tokens, cache.heads, cache.head_dim) or t.stride(2) != 1 or \
-            (cache.heads > 1 and t.stride(1) != cache.head_dim):
-        raise ValueError(f"{name}: expected [tokens, heads, head_dim] with contiguous heads")
-    return t.data_ptr(), (t.stride(0) if batch.tokens > 1 else max(t.stride(0), cache.heads * cache.head_dim)), _ELEMS[t.dtype]
+# The calls below run once per layer and step, next to kernels of a few microseconds: their checks read every attribute
+# once and build nothing that is not needed.
+
+def _kv_raw_stream(stream, device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def _kv_pair(k, v, cache, batch):
-    (kp, ks, ke), (vp, vs, ve) = _kv_rows(k, "k", cache, batch), _kv_rows(v, "v", cache, batch)
-    if ks != vs or ke != ve:
-        raise ValueError("k and v: expected one element type and one row stride")
-    return kp, vp, ke, ks
+    """(pointer of k, pointer of v, element type, row stride) of a step's two [tokens, heads, head_dim] tensors."""
+    shape, stride, dtype = k.shape, k.stride(), k.dtype
+    if v.shape != shape or v.stride() != stride or v.dtype is not dtype:
+        raise ValueError("k and v: expected one shape, one element type and one set of strides")
+    if dtype not in _ELEMS or not (k.is_cuda and v.is_cuda):
+        raise ValueError(f"k, v: expected CUDA tensors of bf16 or fp32, got {dtype}")
+    tokens, heads, dim = batch.tokens, cache.heads, cache.head_dim
+    if shape != (tokens, heads, dim) or stride[2] != 1 or (heads > 1 and stride[1] != dim):
+        raise ValueError("k, v: expected [tokens, heads, head_dim] with contiguous heads")
+    return k.data_ptr(), v.data_ptr(), _ELEMS[dtype], stride[0] if tokens > 1 else heads * dim
 
 
 def kv_append(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, stream=None):
     """Quantises k, v ([tokens, heads, head_dim], bf16 or fp32; column ranges of a fused product's output serve) into the
     cache, request b's i-th row at position start[b] + i."""
     kp, vp, elem, stride = _kv_pair(k, v, cache, batch)
-    _check(lib().tl_kv_append(cache._ref, batch._ref, kp, vp, elem, stride, _stream_ptr(stream)), "tl_kv_append")
+    st = lib().tl_kv_append(cache._ref, batch._ref, kp, vp, elem, stride, _kv_raw_stream(stream, cache._device))
+    if st:
+        _check(st, "tl_kv_append")
 
 
 def kv_read(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, stream=None):
     """Reads the positions kv_append with the same batch writes back into k, v (bf16 or fp32)."""
     kp, vp, elem, stride = _kv_pair(k, v, cache, batch)
-    _check(lib().tl_kv_read(cache._ref, batch._ref, kp, vp, elem, stride, _stream_ptr(stream)), "tl_kv_read")
+    st = lib().tl_kv_read(cache._ref, batch._ref, kp, vp, elem, stride, _kv_raw_stream(stream, cache._device))
+    if st:
+        _check(st, "tl_kv_read")
 
 
 def kv_commit(cache: KvCache, batch: KvBatch, accepted: torch.Tensor, n_accepted: torch.Tensor,
               new_start: torch.Tensor | None = None, stream=None):
     """Moves the rows of accepted[b][i], i < n_accepted[b], to positions start[b] + i; new_start = start + n_accepted."""
-    _cuda(accepted, "accepted", torch.int32, 2)
-    a = _int32(accepted, "accepted", (batch.requests, accepted.shape[1]))
-    n = _int32(n_accepted, "n_accepted", (batch.requests,))
-    s = _int32(new_start, "new_start", (batch.requests,)) if new_start is not None else None
-    _check(lib().tl_kv_commit(cache._ref, batch._ref, a, accepted.shape[1], n, s, _stream_ptr(stream)), "tl_kv_commit")
+    shape, n = accepted.shape, batch.requests
+    if len(shape) != 2:
+        raise ValueError("accepted: expected [requests, n]")
+    a = _int32(accepted, "accepted", (n, shape[1]))
+    st = lib().tl_kv_commit(cache._ref, batch._ref, a, shape[1], _int32(n_accepted, "n_accepted", (n,)),
+                            _int32(new_start, "new_start", (n,)) if new_start is not None else None,
+                            _kv_raw_stream(stream, cache._device))
+    if st:
+        _check(st, "tl_kv_commit")
 
 
 def tree_mask(parents: torch.Tensor, token_offsets: torch.Tensor, mask: torch.Tensor, stream=None):
@@ -575,7 +584,7 @@ def tree_mask(parents: torch.Tensor, token_offsets: torch.Tensor, mask: torch.Te
     m = _int32(mask, "mask", (parents.shape[0], mask.shape[1]))
     _check(lib().tl_tree_mask(_int32(parents, "parents", (mask.shape[0],)),
                               _int32(token_offsets, "token_offsets", (token_offsets.shape[0],)), token_offsets.shape[0] - 1,
-                              mask.shape[0], m, mask.shape[1], _stream_ptr(stream)), "tl_tree_mask")
+                              mask.shape[0], m, mask.shape[1], _kv_raw_stream(stream, mask.device.index)), "tl_tree_mask")
 
 
 def tree_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, out: torch.Tensor, mask: torch.Tensor | None = None,
@@ -583,22 +592,27 @@ def tree_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, out: torch.T
     """out (bf16 [tokens, q_heads, head_dim]) = attention of q over the cache, which holds the step's own rows already.
     mask: int32 [tokens, words] (None: causal within the step's rows); scale: 1 / sqrt(head_dim) by default; lse: fp32
     [tokens, q_heads].  Rows of q and out may be strided."""
-    for t, name in ((q, "q"), (out, "out")):
-        _cuda(t, name, torch.bfloat16, 3)
-        if t.shape[0] != batch.tokens or t.shape[2] != cache.head_dim or t.shape != q.shape or t.stride(2) != 1 or \
-                (t.shape[1] > 1 and t.stride(1) != cache.head_dim):
-            raise ValueError(f"{name}: expected [tokens, q_heads, head_dim] with contiguous heads")
-    heads, words, m = q.shape[1], 0, None
-    wide = heads * cache.head_dim
+    shape, qs, os_ = q.shape, q.stride(), out.stride()
+    tokens, dim = batch.tokens, cache.head_dim
+    if q.dtype is not torch.bfloat16 or out.dtype is not torch.bfloat16 or not (q.is_cuda and out.is_cuda):
+        raise ValueError("q, out: expected CUDA tensors of bf16")
+    if len(shape) != 3 or out.shape != shape or shape[0] != tokens or shape[2] != dim or qs[2] != 1 or os_[2] != 1 or \
+            (shape[1] > 1 and (qs[1] != dim or os_[1] != dim)):
+        raise ValueError("q, out: expected [tokens, q_heads, head_dim] with contiguous heads")
+    heads, words, m, l = shape[1], 0, None, None
+    wide = heads * dim
     if mask is not None:
-        words = _cuda(mask, "mask", torch.int32, 2).shape[1]
-        m = _int32(mask, "mask", (batch.tokens, words))
-    if lse is not None and (_cuda(lse, "lse", torch.float32).shape != q.shape[:2] or not lse.is_contiguous()):
-        raise ValueError("lse: expected a contiguous [tokens, q_heads]")
-    _check(lib().tl_tree_attention(cache._ref, batch._ref, q.data_ptr(), q.stride(0) if batch.tokens > 1 else wide, heads, m,
-                                   words, cache.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
-                                   out.stride(0) if batch.tokens > 1 else wide,
-                                   lse.data_ptr() if lse is not None else None, _stream_ptr(stream)), "tl_tree_attention")
+        words = mask.shape[1]
+        m = _int32(mask, "mask", (tokens, words))
+    if lse is not None:
+        if _cuda(lse, "lse", torch.float32).shape != shape[:2] or not lse.is_contiguous():
+            raise ValueError("lse: expected a contiguous [tokens, q_heads]")
+        l = lse.data_ptr()
+    st = lib().tl_tree_attention(cache._ref, batch._ref, q.data_ptr(), qs[0] if tokens > 1 else wide, heads, m, words,
+                                 dim ** -0.5 if scale is None else scale, out.data_ptr(), os_[0] if tokens > 1 else wide, l,
+                                 _kv_raw_stream(stream, cache._device))
+    if st:
+        _check(st, "tl_tree_attention")
 
 
 def tree_attention_workspace_bytes(cache: KvCache, batch: KvBatch, q_heads: int) -> int:
@@ -614,21 +628,24 @@ def tree_verify(target: torch.Tensor, draft: torch.Tensor | None, tokens: torch.
     [tokens]; accept: fp32 [tokens] and sample: fp32 [requests], uniform in [0, 1).  Written: accepted int32 [requests, n]
     (rows kept within the request, root first, then -1), n_accepted and next_token int32 [requests].
     """
-    rows, vocab = _cuda(target, "target", torch.float32, 2).shape
-    requests = token_offsets.shape[0] - 1
-    if draft is not None and _cuda(draft, "draft", torch.float32, 2).shape != target.shape:
-        raise ValueError("draft: expected the shape of target")
-    for t, name in ((target, "target"), (draft, "draft")):
-        if t is not None and t.stride(1) != 1 and vocab > 1:
-            raise ValueError(f"{name}: expected contiguous rows")
+    shape, ts, f32 = target.shape, target.stride(), torch.float32
+    rows, vocab = shape
+    requests, most = token_offsets.shape[0] - 1, accepted.shape[1]
+    if target.dtype is not f32 or not target.is_cuda or (ts[1] != 1 and vocab > 1):
+        raise ValueError("target: expected a CUDA tensor of fp32 with contiguous rows")
+    dp = ds = 0
+    if draft is not None:
+        ds = draft.stride()
+        if draft.dtype is not f32 or not draft.is_cuda or draft.shape != shape or (ds[1] != 1 and vocab > 1):
+            raise ValueError("draft: expected target's shape, type and contiguous rows")
+        dp, ds = draft.data_ptr(), max(ds[0], vocab)
     for t, name, n in ((accept, "accept", rows), (sample, "sample", requests)):
-        if _cuda(t, name, torch.float32).shape != (n,) or not t.is_contiguous():
-            raise ValueError(f"{name}: expected a contiguous tensor of {n} numbers")
-    _cuda(accepted, "accepted", torch.int32, 2)
-    _check(lib().tl_tree_verify(target.data_ptr(), max(target.stride(0), vocab), draft.data_ptr() if draft is not None else None,
-                                max(draft.stride(0), vocab) if draft is not None else 0, vocab,
-                                _int32(tokens, "tokens", (rows,)), _int32(parents, "parents", (rows,)),
-                                _int32(token_offsets, "token_offsets", (requests + 1,)), requests, rows, accept.data_ptr(),
-                                sample.data_ptr(), _int32(accepted, "accepted", (requests, accepted.shape[1])),
-                                accepted.shape[1], _int32(n_accepted, "n_accepted", (requests,)),
-                                _int32(next_token, "next_token", (requests,)), _stream_ptr(stream)), "tl_tree_verify")
+        if t.dtype is not f32 or not t.is_cuda or t.shape != (n,) or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous CUDA tensor of {n} fp32 numbers")
+    st = lib().tl_tree_verify(target.data_ptr(), max(ts[0], vocab), dp, ds, vocab, _int32(tokens, "tokens", (rows,)),
+                              _int32(parents, "parents", (rows,)), _int32(token_offsets, "token_offsets", (requests + 1,)),
+                              requests, rows, accept.data_ptr(), sample.data_ptr(),
+                              _int32(accepted, "accepted", (requests, most)), most, _int32(n_accepted, "n_accepted", (requests,)),
+                              _int32(next_token, "next_token", (requests,)), _kv_raw_stream(stream, target.device.index))
+    if st:
+        _check(st, "tl_tree_verify")
