@@ -130,20 +130,72 @@ __device__ __forceinline__ void store8(char* dst, bool f32, const float (&x)[8])
 // context of 22000 tokens, 8 heads, INT8 to bf16 at 2.1 TB/s, the loads of a warp waiting one by one.)
 constexpr int kCopyThreads = 256, kCopyAhead = 4;
 
-// Where the warp's row lies in the cache, and its request; false when no request owns the row.
+// Where the warp's row lies in the cache (offsets of head 0, the same for keys and values); false when no request owns the
+// row.
 struct KvRowPlace {
-    char* base;                 // of head 0, or null without a page
-    float* scale;
+    bool page;                  // there is one
+    int64_t at, scale_at;       // bytes, floats
 };
-__device__ __forceinline__ bool kv_locate_row(const KvCopyParams& p, int row, int which, KvRowPlace* out) {
-    const int b = warp_request_of(p.batch, row);
-    if (b >= p.batch.requests) return false;
-    const KvRequest r = kv_request(p.batch, p.cache.page_shift, b);
-    if (row < r.first || row >= r.first + r.n) return false;
-    out->scale = nullptr;
-    out->base = kv_row(p.cache, p.batch, b, r.start + (row - r.first), which, 0, p.cache.scale[0] ? &out->scale : nullptr);
+__device__ __forceinline__ bool kv_locate_row(const KvCopyParams& p, int row, KvRowPlace* out) {
+    // the request that owns the row, looked for 32 at a time; each lane has its request's data at hand (a look at them once
+    // the owner is known would be one more round trip)
+    const KvBatchView& bv = p.batch;
+    KvRequest r = {};
+    int b = bv.requests;
+    for (int b0 = 0; b0 < bv.requests; b0 += 32) {
+        const int mine = min(b0 + int(lane_id()), bv.requests - 1);
+        const KvRequest q = kv_request(bv, p.cache.page_shift, mine);
+        const uint32_t owner = __ballot_sync(0xffffffffu, b0 + int(lane_id()) < bv.requests && row >= q.first && row < q.first + q.n);
+        if (owner) {
+            const int l = __ffs(int(owner)) - 1;
+            b = b0 + l;
+            r.first = __shfl_sync(0xffffffffu, q.first, l);
+            r.start = __shfl_sync(0xffffffffu, q.start, l);
+            break;
+        }
+    }
+    if (b >= bv.requests) return false;
+    const int pos = r.start + (row - r.first);
+    out->page = false;
+    out->at = out->scale_at = 0;
+    if (pos >= kv_room(p.batch, p.cache.page_shift)) return true;
+    const int64_t page = p.batch.page_table[int64_t(b) * p.batch.table_stride + (pos >> p.cache.page_shift)];
+    const int line = pos & ((1 << p.cache.page_shift) - 1);
+    out->page = page >= 0 && page < p.cache.pages;
+    if (!out->page) return true;
+    out->at = page * p.cache.page_stride + line * p.cache.token_stride;
+    out->scale_at = page * p.cache.scale_page_stride + line;
     return true;
 }
+
+// Eight codes of a lane and the values they stand for.
+template <int kFmt>
+struct KvCodes {
+    using type = uint2;
+    __device__ static void expand(uint2 c, float s, float (&x)[8]) {
+        uint32_t h[4];
+        codes4_to_f16<kFmt>(c.x, h[0], h[1]);
+        codes4_to_f16<kFmt>(c.y, h[2], h[3]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[e]));
+            x[2 * e] = f.x * s;
+            x[2 * e + 1] = f.y * s;
+        }
+    }
+};
+template <>
+struct KvCodes<TL_KV_BF16> {
+    using type = uint4;
+    __device__ static void expand(uint4 c, float, float (&x)[8]) {
+        const uint32_t u[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[2 * e] = __uint_as_float(u[e] << 16);
+            x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+        }
+    }
+};
 
 template <int kFmt, int kDim, bool kF32>
 __global__ void __launch_bounds__(kCopyThreads) kv_append_kernel(const KvCopyParams p) {
@@ -156,14 +208,15 @@ __global__ void __launch_bounds__(kCopyThreads) kv_append_kernel(const KvCopyPar
     const int64_t warps = int64_t(gridDim.x) * (kCopyThreads / 32);
     for (int64_t w = blockIdx.x * int64_t(kCopyThreads / 32) + threadIdx.x / 32; w < total; w += warps) {
         const int chunk = int(w % chunks), which = int(w / chunks) & 1, row = int(w / chunks / 2), head0 = chunk * kPerWarp * kCopyAhead + sub;
-        const char* const src = p.rows[which] + int64_t(row) * p.row_stride + (int64_t(head0) * kDim + l * 8) * kItem;
-        float x[kCopyAhead][8];
+        // (as they come: 16 or 32 bytes of a head's row)
+        struct Raw { uint4 v[kF32 ? 2 : 1]; } raw[kCopyAhead];
 #pragma unroll
         for (int i = 0; i < kCopyAhead; ++i)
-            if (head0 + i * kPerWarp < heads) load8(src + int64_t(i) * kPerWarp * kDim * kItem, kF32, x[i]);
+            if (head0 + i * kPerWarp < heads)
+                raw[i] = *reinterpret_cast<const Raw*>(p.rows[which] + int64_t(row) * p.row_stride + (int64_t(head0 + i * kPerWarp) * kDim + l * 8) * kItem);
         KvRowPlace at;
-        if (!kv_locate_row(p, row, which, &at)) continue;
-        if (!at.base) {
+        if (!kv_locate_row(p, row, &at)) continue;
+        if (!at.page) {
             if (lane_id() == 0) atomicCAS(p.status, 0u, kBadPage);
             continue;
         }
@@ -171,15 +224,17 @@ __global__ void __launch_bounds__(kCopyThreads) kv_append_kernel(const KvCopyPar
         for (int i = 0; i < kCopyAhead; ++i) {
             const int head = head0 + i * kPerWarp;
             if (head >= heads) continue;                      // (whole groups leave together; no shuffle spans groups)
-            char* const dst = at.base + int64_t(head) * p.cache.head_stride;
+            char* const dst = p.cache.base[which] + at.at + int64_t(head) * p.cache.head_stride;
+            float x[8];
+            load8(reinterpret_cast<const char*>(&raw[i]), kF32, x);
             if (kFmt == TL_KV_BF16) {
-                store8(dst + l * 16, false, x[i]);
+                store8(dst + l * 16, false, x);
                 continue;
             }
             // the largest magnitude, as bits: a NaN's pattern is above an infinity's, so either makes the scale NaN
             uint32_t top = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[i][e]) & 0x7fffffffu);
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
             const uint32_t group = (kLanes == 32 ? 0xffffffffu : ((1u << kLanes) - 1u) << (sub * kLanes));
 #pragma unroll
             for (int d = kLanes / 2; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(group, top, d));
@@ -188,8 +243,20 @@ __global__ void __launch_bounds__(kCopyThreads) kv_append_kernel(const KvCopyPar
             uint32_t lo = 0, hi = 0;
             if (finite && s > 0.0f) {
                 float y[8];
+                if (s > 0x1p-90f && s < 0x1p90f) {
+                    // x / s with the row's reciprocal: given the correctly rounded 1 / s, one FMA correction of x * (1 / s) is
+                    // the correctly rounded quotient (Markstein 1990).  The remainder must not underflow: it is at least
+                    // 2^-35 s where the quotient is 2^-11 or more, and below that any quotient rounds to code 0.
+                    const float inv = __frcp_rn(s);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = __fdiv_rn(x[i][e], s);
+                    for (int e = 0; e < 8; ++e) {
+                        const float q = __fmul_rn(x[e], inv);
+                        y[e] = __fmaf_rn(__fmaf_rn(-q, s, x[e]), inv, q);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = __fdiv_rn(x[e], s);
+                }
                 if (kFmt == TL_KV_E4M3) {
                     // (the saturating conversion keeps the last bit of a quotient just above 448)
                     auto two = [](float a, float c) -> uint32_t {
@@ -206,7 +273,7 @@ __global__ void __launch_bounds__(kCopyThreads) kv_append_kernel(const KvCopyPar
                 }
             }
             *reinterpret_cast<uint2*>(dst + l * 8) = make_uint2(lo, hi);
-            if (l == 0) at.scale[int64_t(head) * p.cache.scale_head_stride] = s;
+            if (l == 0) p.cache.scale[which][at.scale_at + int64_t(head) * p.cache.scale_head_stride] = s;
         }
     }
 }
@@ -223,48 +290,26 @@ __global__ void __launch_bounds__(kCopyThreads) kv_read_kernel(const KvCopyParam
     for (int64_t w = blockIdx.x * int64_t(kCopyThreads / 32) + threadIdx.x / 32; w < total; w += warps) {
         const int chunk = int(w % chunks), which = int(w / chunks) & 1, row = int(w / chunks / 2), head0 = chunk * kPerWarp * kCopyAhead + sub;
         KvRowPlace at;
-        if (!kv_locate_row(p, row, which, &at)) continue;
-        if (!at.base && lane_id() == 0) atomicCAS(p.status, 0u, kBadPage);
-        uint4 c[kCopyAhead];
+        if (!kv_locate_row(p, row, &at)) continue;
+        if (!at.page && lane_id() == 0) atomicCAS(p.status, 0u, kBadPage);
+        using Codes = typename KvCodes<kFmt>::type;
+        Codes c[kCopyAhead];
         float s[kCopyAhead];
 #pragma unroll
         for (int i = 0; i < kCopyAhead; ++i) {
             const int head = head0 + i * kPerWarp;
-            c[i] = make_uint4(0, 0, 0, 0);
+            c[i] = Codes{};
             s[i] = 0.0f;
-            if (head >= heads || !at.base) continue;
-            const char* const src = at.base + int64_t(head) * p.cache.head_stride;
-            if (kFmt == TL_KV_BF16) {
-                c[i] = *reinterpret_cast<const uint4*>(src + l * 16);
-            } else {
-                const uint2 h = *reinterpret_cast<const uint2*>(src + l * 8);
-                c[i].x = h.x, c[i].y = h.y;
-                s[i] = at.scale[int64_t(head) * p.cache.scale_head_stride];
-            }
+            if (head >= heads || !at.page) continue;
+            c[i] = *reinterpret_cast<const Codes*>(p.cache.base[which] + at.at + int64_t(head) * p.cache.head_stride + l * int(sizeof(Codes)));
+            if (kFmt != TL_KV_BF16) s[i] = p.cache.scale[which][at.scale_at + int64_t(head) * p.cache.scale_head_stride];
         }
         char* const dst = p.rows[which] + int64_t(row) * p.row_stride + (int64_t(head0) * kDim + l * 8) * kItem;
 #pragma unroll
         for (int i = 0; i < kCopyAhead; ++i) {
             if (head0 + i * kPerWarp >= heads) continue;
             float x[8];
-            if (kFmt == TL_KV_BF16) {
-                const uint32_t u[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[2 * e] = __uint_as_float(u[e] << 16);
-                    x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
-                }
-            } else {
-                uint32_t h[4];
-                codes4_to_f16<kFmt>(c[i].x, h[0], h[1]);
-                codes4_to_f16<kFmt>(c[i].y, h[2], h[3]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[e]));
-                    x[2 * e] = f.x * s[i];
-                    x[2 * e + 1] = f.y * s[i];
-                }
-            }
+            KvCodes<kFmt>::expand(c[i], s[i], x);
             store8(dst + int64_t(i) * kPerWarp * kDim * kItem, kF32, x);
         }
     }

@@ -233,3 +233,23 @@ def test_tree_mask(counts, words):
     tl.tree_mask(parents, offs, mask)
     want = torch.cat([ref.tree_bits(t, words) for t in trees if t])
     assert torch.equal(mask.cpu(), want)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_codes_are_those_of_the_exact_quotient(fmt):
+    # A million quotients, bf16 (whose ratios often lie on, or next to, the middle between two codes) and fp32, at scales
+    # from the smallest normal numbers to the largest: every code is the division's.
+    from paper_2607_04031_b200 import binding as tl
+    for dtype in (torch.bfloat16, torch.float32):
+        g = torch.Generator().manual_seed(12)
+        x = torch.randn(4096, 1, 256, generator=g) * torch.exp2(torch.randint(-120, 120, (4096, 1, 1), generator=g).float())
+        x = x.to(dtype)
+        pool = ref.Pool(fmt, 1, 256, 64, [4096], seed=1)
+        batch = tl.kv_batch(pool.table.cuda(), torch.zeros(1, dtype=torch.int32, device="cuda"),
+                            torch.tensor([0, 4096], dtype=torch.int32, device="cuda"), 4096)
+        dev = pool.device("cuda:0")
+        tl.kv_append(tl.kv_cache(*dev), batch, x.cuda(), x.cuda())
+        tl.device_status()
+        pool.write(0, torch.arange(4096), x, x)
+        for got, want in zip(dev, (pool.k, pool.v, pool.ks, pool.vs)):
+            assert _same(got, want)
