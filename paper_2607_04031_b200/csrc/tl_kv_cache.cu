@@ -202,12 +202,11 @@ __global__ void __launch_bounds__(kCopyThreads) kv_append_kernel(const KvCopyPar
     pdl_wait();
     pdl_launch_dependents();
     constexpr int kLanes = kDim / 8, kPerWarp = 32 / kLanes, kItem = kF32 ? 4 : 2;
-    const int heads = p.cache.heads, chunks = (heads + kPerWarp * kCopyAhead - 1) / (kPerWarp * kCopyAhead);
-    const int64_t total = int64_t(p.batch.tokens) * 2 * chunks;
-    const int sub = int(lane_id()) / kLanes, l = int(lane_id()) % kLanes;
-    const int64_t warps = int64_t(gridDim.x) * (kCopyThreads / 32);
-    for (int64_t w = blockIdx.x * int64_t(kCopyThreads / 32) + threadIdx.x / 32; w < total; w += warps) {
-        const int chunk = int(w % chunks), which = int(w / chunks) & 1, row = int(w / chunks / 2), head0 = chunk * kPerWarp * kCopyAhead + sub;
+    const int heads = p.cache.heads, which = int(blockIdx.y) & 1;
+    const int sub = int(lane_id()) / kLanes, l = int(lane_id()) % kLanes, head0 = int(blockIdx.y >> 1) * kPerWarp * kCopyAhead + sub;
+    const int64_t step = int64_t(gridDim.x) * (kCopyThreads / 32);
+    for (int64_t at_row = blockIdx.x * int64_t(kCopyThreads / 32) + threadIdx.x / 32; at_row < p.batch.tokens; at_row += step) {
+        const int row = int(at_row);
         // (as they come: 16 or 32 bytes of a head's row)
         struct Raw { uint4 v[kF32 ? 2 : 1]; } raw[kCopyAhead];
 #pragma unroll
@@ -283,12 +282,11 @@ __global__ void __launch_bounds__(kCopyThreads) kv_read_kernel(const KvCopyParam
     pdl_wait();
     pdl_launch_dependents();
     constexpr int kLanes = kDim / 8, kPerWarp = 32 / kLanes, kItem = kF32 ? 4 : 2;
-    const int heads = p.cache.heads, chunks = (heads + kPerWarp * kCopyAhead - 1) / (kPerWarp * kCopyAhead);
-    const int64_t total = int64_t(p.batch.tokens) * 2 * chunks;
-    const int sub = int(lane_id()) / kLanes, l = int(lane_id()) % kLanes;
-    const int64_t warps = int64_t(gridDim.x) * (kCopyThreads / 32);
-    for (int64_t w = blockIdx.x * int64_t(kCopyThreads / 32) + threadIdx.x / 32; w < total; w += warps) {
-        const int chunk = int(w % chunks), which = int(w / chunks) & 1, row = int(w / chunks / 2), head0 = chunk * kPerWarp * kCopyAhead + sub;
+    const int heads = p.cache.heads, which = int(blockIdx.y) & 1;
+    const int sub = int(lane_id()) / kLanes, l = int(lane_id()) % kLanes, head0 = int(blockIdx.y >> 1) * kPerWarp * kCopyAhead + sub;
+    const int64_t step = int64_t(gridDim.x) * (kCopyThreads / 32);
+    for (int64_t at_row = blockIdx.x * int64_t(kCopyThreads / 32) + threadIdx.x / 32; at_row < p.batch.tokens; at_row += step) {
+        const int row = int(at_row);
         KvRowPlace at;
         if (!kv_locate_row(p, row, &at)) continue;
         if (!at.page && lane_id() == 0) atomicCAS(p.status, 0u, kBadPage);
@@ -461,10 +459,10 @@ static int kv_copy(bool append, const tl_kv_cache* cache, const tl_kv_batch* bat
         case TL_KV_E4M3: kernel = f32 ? pick_copy<TL_KV_E4M3, true>(append, cache->head_dim) : pick_copy<TL_KV_E4M3, false>(append, cache->head_dim); break;
         default: kernel = f32 ? pick_copy<TL_KV_INT8, true>(append, cache->head_dim) : pick_copy<TL_KV_INT8, false>(append, cache->head_dim); break;
     }
-    const int64_t per_warp = int64_t(kCopyAhead) * (32 / (cache->head_dim / 8));
-    const int64_t blocks = ceil_div(int64_t(p.batch.tokens) * 2 * ceil_div(cache->heads, per_warp), kCopyThreads / 32);
-    const int64_t grid = std::min<int64_t>(blocks, int64_t(dev().sm_count) * 8 * 4);
-    return kv_launch(kernel, dim3(unsigned(grid)), kCopyThreads, static_cast<cudaStream_t>(cuda_stream), p);
+    const int64_t chunks = ceil_div(cache->heads, int64_t(kCopyAhead) * (32 / (cache->head_dim / 8)));
+    if (2 * chunks > 65535) return TL_ERR_UNSUPPORTED;
+    const int64_t blocks = std::min<int64_t>(ceil_div(p.batch.tokens, kCopyThreads / 32), std::max<int64_t>(int64_t(dev().sm_count) * 16 / chunks, 1));
+    return kv_launch(kernel, dim3(unsigned(blocks), unsigned(2 * chunks)), kCopyThreads, static_cast<cudaStream_t>(cuda_stream), p);
 }
 
 }  // namespace tl
