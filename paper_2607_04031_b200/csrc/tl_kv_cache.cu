@@ -232,8 +232,15 @@ __global__ void __launch_bounds__(kCopyThreads) kv_append_kernel(const KvCopyPar
             }
             // the largest magnitude, as bits: a NaN's pattern is above an infinity's, so either makes the scale NaN
             uint32_t top = 0;
+            if (kF32) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+                for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+            } else {
+                const uint32_t u[4] = {raw[i].v[0].x, raw[i].v[0].y, raw[i].v[0].z, raw[i].v[0].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = __vmaxu2(top, u[e] & 0x7fff7fffu);          // two bf16 patterns at a time
+                top = max(top & 0xffff0000u, top << 16);
+            }
             const uint32_t group = (kLanes == 32 ? 0xffffffffu : ((1u << kLanes) - 1u) << (sub * kLanes));
 #pragma unroll
             for (int d = kLanes / 2; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(group, top, d));
@@ -266,9 +273,12 @@ __global__ void __launch_bounds__(kCopyThreads) kv_append_kernel(const KvCopyPar
                     lo = two(y[0], y[1]) | two(y[2], y[3]) << 16;
                     hi = two(y[4], y[5]) | two(y[6], y[7]) << 16;
                 } else {
-                    auto one = [](float a) -> uint32_t { return uint32_t(min(max(__float2int_rn(a), -127), 127)) & 0xffu; };
-                    lo = one(y[0]) | one(y[1]) << 8 | one(y[2]) << 16 | one(y[3]) << 24;
-                    hi = one(y[4]) | one(y[5]) << 8 | one(y[6]) << 16 | one(y[7]) << 24;
+                    // |y| <= 127 (1 + 2^-22), so rounding needs no clamp; 1.5 x 2^23 leaves the integer in the low bits
+                    uint32_t z[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = __float_as_uint(__fadd_rn(y[e], 12582912.0f));
+                    lo = __byte_perm(__byte_perm(z[0], z[1], 0x0040), __byte_perm(z[2], z[3], 0x0040), 0x5410);
+                    hi = __byte_perm(__byte_perm(z[4], z[5], 0x0040), __byte_perm(z[6], z[7], 0x0040), 0x5410);
                 }
             }
             *reinterpret_cast<uint2*>(dst + l * 8) = make_uint2(lo, hi);
