@@ -578,7 +578,7 @@ size_t tl_tree_attention_workspace_bytes(const tl_kv_cache* cache, const tl_kv_b
  * vocabulary are fp64.
  *   d_accepted    int32 [requests][accepted_stride]: rows kept, within the request, root first, then -1.
  *   d_n_accepted  int32 [requests]: how many (0 for a request without rows).  d_next: int32 [requests] (-1 then).
- * A path ends at accepted_stride rows (>= 1): the last of them is treated as one without children.  Asynchronous.
+ * vocab is at most 2^30.  A path ends at accepted_stride rows (>= 1): the last of them is treated as one without children.  Asynchronous.
  */
 int tl_tree_verify(const float* d_target, int64_t target_stride, const float* d_draft, int64_t draft_stride, int64_t vocab,
                    const int32_t* d_tokens, const int32_t* d_parents, const int32_t* d_token_offsets, int requests,

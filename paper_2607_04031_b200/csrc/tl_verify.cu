@@ -35,6 +35,7 @@ struct VerifyParams {
 struct VerifySmem {
     double total[2][8];                  // [pass parity][rank]: this CTA's copy of the slices' sums
     double part[kVerifyWarps];           // the warps' sums of the last pass
+    double row[32];                      // sums of 32 ids each, when the draw looks for its id
     double mass[kVerifyTries];           // S before each refused draft of the node
     int32_t gone[kVerifyTries];          // their tokens
     int32_t parent[kVerifyRows];
@@ -53,7 +54,7 @@ __device__ __forceinline__ void st_cluster_f64(uint32_t cluster_addr, double v) 
 }
 
 template <bool kDraft>
-__global__ void __launch_bounds__(kVerifyThreads) tree_verify_kernel(const VerifyParams p, int cluster) {
+__global__ void __launch_bounds__(kVerifyThreads, 2) tree_verify_kernel(const VerifyParams p, int cluster) {
     __shared__ VerifySmem sm;
     pdl_wait();
     pdl_launch_dependents();
@@ -98,14 +99,16 @@ __global__ void __launch_bounds__(kVerifyThreads) tree_verify_kernel(const Verif
     if (cluster > 1) cluster_sync();
     else __syncthreads();
 
-    const int64_t slice = (p.vocab + cluster - 1) / cluster;
-    const int64_t s0 = min(int64_t(rank) * slice, p.vocab), s1 = min(s0 + slice, p.vocab);
-    const int64_t per_warp = ((s1 - s0 + kVerifyWarps - 1) / kVerifyWarps + 31) / 32 * 32;
-    const int64_t w0 = min(s0 + int64_t(warp) * per_warp, s1), w1 = min(w0 + per_warp, s1);
+    // (ids fit 32 bits with room for the roundings below: the host bounds the vocabulary)
+    const int vocab = int(p.vocab);
+    const int slice = ((vocab + cluster - 1) / cluster + 3) / 4 * 4;
+    const int s0 = min(rank * slice, vocab), s1 = min(s0 + slice, vocab);
+    const int per_warp = ((s1 - s0 + kVerifyWarps - 1) / kVerifyWarps + 31) / 32 * 32;
+    const int w0 = min(s0 + warp * per_warp, s1), w1 = min(w0 + per_warp, s1);
     int parity = 0, node = 0, length = 1, tries = 0;
 
     // the residual at id j of the node's rows, after `tries` refused drafts
-    auto value = [&](const float* prow, const float* qrow, int64_t j, float pj, float qj) -> double {
+    auto value = [&](int j, float pj, float qj) -> double {
         double r = positive(pj);
         if (kDraft) {
             const double q = positive(qj);
@@ -119,19 +122,61 @@ __global__ void __launch_bounds__(kVerifyThreads) tree_verify_kernel(const Verif
     auto pass = [&]() -> double {
         const float* prow = target + int64_t(node) * p.target_stride;
         const float* qrow = kDraft && tries > 0 ? draft + int64_t(node) * p.draft_stride : nullptr;
+        // One term of the sum; the common cases (no refused draft, one, none of this warp's ids refused) have loops of their
+        // own: the general one costs several times their instructions, and instructions are what a pass is made of.
         double sum = 0.0;
-        constexpr int kUnroll = 8;
-        for (int64_t j0 = w0; j0 < w1; j0 += 32 * kUnroll) {
-            float pj[kUnroll], qj[kUnroll];
+        auto sweep = [&](auto term) {
+            int j0 = w0;
+            if (((reinterpret_cast<uintptr_t>(prow) | reinterpret_cast<uintptr_t>(qrow)) & 15u) == 0) {
+                constexpr int kUnroll = 2;                   // x 4 ids x 32 lanes (w0 is a multiple of 4)
+                for (; j0 + 128 * kUnroll <= w1; j0 += 128 * kUnroll) {
+                    float4 pj[kUnroll], qj[kUnroll];
 #pragma unroll
-            for (int e = 0; e < kUnroll; ++e) {
-                const int64_t j = j0 + e * 32 + lane;
-                pj[e] = j < w1 ? prow[j] : 0.0f;
-                qj[e] = kDraft && qrow && j < w1 ? qrow[j] : 0.0f;
+                    for (int e = 0; e < kUnroll; ++e) {
+                        const int j = j0 + e * 128 + lane * 4;
+                        pj[e] = *reinterpret_cast<const float4*>(prow + j);
+                        qj[e] = qrow ? *reinterpret_cast<const float4*>(qrow + j) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+#pragma unroll
+                    for (int e = 0; e < kUnroll; ++e) {
+                        const int j = j0 + e * 128 + lane * 4;
+                        sum += (term(j, pj[e].x, qj[e].x) + term(j + 1, pj[e].y, qj[e].y)) + (term(j + 2, pj[e].z, qj[e].z) + term(j + 3, pj[e].w, qj[e].w));
+                    }
+                }
             }
+            constexpr int kUnroll = 8;
+            for (; j0 + 32 * kUnroll <= w1; j0 += 32 * kUnroll) {
+                float pj[kUnroll], qj[kUnroll];
 #pragma unroll
-            for (int e = 0; e < kUnroll; ++e) sum += value(prow, qrow, j0 + e * 32 + lane, pj[e], qj[e]);
-        }
+                for (int e = 0; e < kUnroll; ++e) {
+                    pj[e] = prow[j0 + e * 32 + lane];
+                    qj[e] = qrow ? qrow[j0 + e * 32 + lane] : 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < kUnroll; ++e) sum += term(j0 + e * 32 + lane, pj[e], qj[e]);
+            }
+            for (int j = j0 + lane; j < w1; j += 32) sum += term(j, prow[j], qrow ? qrow[j] : 0.0f);
+        };
+        int special = 0, gone[4] = {-1, -1, -1, -1};         // refused ids among this warp's
+        if (!kDraft)
+            for (int k = 0; k < tries; ++k) {
+                const int id = sm.gone[k];
+                if (id < w0 || id >= w1) continue;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) gone[e] = special == e ? id : gone[e];
+                ++special;
+            }
+        if (kDraft ? tries == 0 : special == 0) sweep([](int, float pj, float) { return positive(pj); });
+        else if (kDraft && tries == 1)                       // max(p - q, 0), the mass being 1
+            sweep([](int, float pj, float qj) {
+                const float pz = fmaxf(pj, 0.0f), qz = fmaxf(qj, 0.0f);
+                return pz > qz ? double(pz) - double(qz) : 0.0;
+            });
+        else if (!kDraft && special <= 4)
+            sweep([&](int j, float pj, float) {
+                return positive(j == gone[0] || j == gone[1] || j == gone[2] || j == gone[3] ? 0.0f : pj);
+            });
+        else sweep(value);
         sum = warp_sum_f64(sum);
         __syncthreads();                                     // the last pass's sums have been read
         if (lane == 0) sm.part[warp] = sum;
@@ -177,7 +222,7 @@ __global__ void __launch_bounds__(kVerifyThreads) tree_verify_kernel(const Verif
                     token = p.tokens[first + c], u = p.accept[first + c];
                     gather(c, node, token, pc, qc);
                 }
-                const double r = value(nullptr, nullptr, token, pc, qc), q = positive(qc);
+                const double r = value(token, pc, qc), q = positive(qc);
                 if (double(u) * q * mass < r) {
                     next = c;
                     break;
@@ -252,38 +297,58 @@ __global__ void __launch_bounds__(kVerifyThreads) tree_verify_kernel(const Verif
                 }
                 run += s;
             }
-            if (w == warp) {
-                const float* prow = target + int64_t(node) * p.target_stride;
-                const float* qrow = kDraft && tries > 0 ? draft + int64_t(node) * p.draft_stride : nullptr;
-                double sum = from;
-                int64_t found = -1, last = -1;
-                constexpr int kUnroll = 8;
-                for (int64_t j0 = w0; j0 < w1 && found < 0; j0 += 32 * kUnroll) {
-                    float pj[kUnroll], qj[kUnroll];
+            // All warps of the CTA look through warp w's ids, 32 rows of 32 at a time, two rows a warp: the rows' sums to shared
+            // memory, one scan over them, and one over the row that holds the answer.  (The values are in the second-level
+            // cache by now.)
+            const float* prow = target + int64_t(node) * p.target_stride;
+            const float* qrow = kDraft && tries > 0 ? draft + int64_t(node) * p.draft_stride : nullptr;
+            const int f0 = min(s0 + w * per_warp, s1), f1 = min(f0 + per_warp, s1);
+            auto scan = [&](double v) {                      // inclusive running sum over the lanes
 #pragma unroll
-                    for (int e = 0; e < kUnroll; ++e) {
-                        const int64_t j = j0 + e * 32 + lane;
-                        pj[e] = j < w1 ? prow[j] : 0.0f;
-                        qj[e] = kDraft && qrow && j < w1 ? qrow[j] : 0.0f;
-                    }
-#pragma unroll
-                    for (int e = 0; e < kUnroll; ++e) {
-                        if (found >= 0) break;
-                        const double r = value(prow, qrow, j0 + e * 32 + lane, pj[e], qj[e]);
-                        double run_to = r;                   // inclusive running sum over the lanes
-#pragma unroll
-                        for (int d = 1; d < 32; d <<= 1) {
-                            const double up = __shfl_up_sync(0xffffffffu, run_to, d);
-                            if (lane >= d) run_to += up;
-                        }
-                        const uint32_t hit = __ballot_sync(0xffffffffu, sum + run_to > t && r > 0.0);
-                        const uint32_t some = __ballot_sync(0xffffffffu, r > 0.0);
-                        if (some) last = j0 + e * 32 + 31 - __clz(int(some));
-                        if (hit) found = j0 + e * 32 + __ffs(int(hit)) - 1;
-                        sum += __shfl_sync(0xffffffffu, run_to, 31);
-                    }
+                for (int d = 1; d < 32; d <<= 1) {
+                    const double up = __shfl_up_sync(0xffffffffu, v, d);
+                    if (lane >= d) v += up;
                 }
-                if (lane == 0) p.next[b] = int32_t(found >= 0 ? found : last);
+                return v;
+            };
+            double sum = from, row_from = from;
+            int row = -1;                                    // the last row with anything in it, or the one that exceeds t
+            for (int j0 = f0; j0 < f1; j0 += 1024) {
+                float pj[2], qj[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int j = j0 + (warp + e * kVerifyWarps) * 32 + lane;
+                    pj[e] = j < f1 ? prow[j] : 0.0f;
+                    qj[e] = kDraft && qrow && j < f1 ? qrow[j] : 0.0f;
+                }
+                double v[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) v[e] = warp_sum_f64(value(j0 + (warp + e * kVerifyWarps) * 32 + lane, pj[e], qj[e]));
+                __syncthreads();                             // the last rows' sums have been read
+                if (lane == 0) {
+                    sm.row[warp] = v[0];
+                    sm.row[warp + kVerifyWarps] = v[1];
+                }
+                __syncthreads();
+                const double mine = sm.row[lane], to = scan(mine);
+                const uint32_t some = __ballot_sync(0xffffffffu, mine > 0.0), over = __ballot_sync(0xffffffffu, sum + to > t && mine > 0.0);
+                if (some) {
+                    const int k = over ? __ffs(int(over)) - 1 : 31 - __clz(int(some));
+                    row = j0 + k * 32;
+                    row_from = sum + __shfl_sync(0xffffffffu, to - mine, k);
+                }
+                if (over) break;
+                sum += __shfl_sync(0xffffffffu, to, 31);
+            }
+            if (warp == 0) {
+                int found = -1;
+                if (row >= 0) {
+                    const int j = row + lane;
+                    const double r = j < f1 ? value(j, prow[j], kDraft && qrow ? qrow[j] : 0.0f) : 0.0, to = scan(r);
+                    const uint32_t hit = __ballot_sync(0xffffffffu, row_from + to > t && r > 0.0), any = __ballot_sync(0xffffffffu, r > 0.0);
+                    found = row + (hit ? __ffs(int(hit)) - 1 : 31 - __clz(int(any | 1u)));
+                }
+                if (lane == 0) p.next[b] = found;
             }
         }
     }
@@ -300,7 +365,7 @@ int tl_tree_verify(const float* d_target, int64_t target_stride, const float* d_
                    int tokens, const float* d_accept, const float* d_sample, int32_t* d_accepted,
                    int64_t accepted_stride, int32_t* d_n_accepted, int32_t* d_next, void* cuda_stream) {
     using namespace tl;
-    if (requests < 0 || tokens < 0 || vocab < 1 || vocab > INT32_MAX || accepted_stride < 1) return TL_ERR_INVALID_ARG;
+    if (requests < 0 || tokens < 0 || vocab < 1 || vocab > (1 << 30) || accepted_stride < 1) return TL_ERR_INVALID_ARG;
     if (requests == 0) return TL_OK;
     if (!d_token_offsets || !d_accepted || !d_n_accepted || !d_next || !d_sample) return TL_ERR_INVALID_ARG;
     if (tokens > 0 && (!d_target || !d_tokens || !d_parents || !d_accept)) return TL_ERR_INVALID_ARG;
