@@ -172,7 +172,15 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) tree_verify_kernel(const Ve
                 const float pz = fmaxf(pj, 0.0f), qz = fmaxf(qj, 0.0f);
                 return pz > qz ? double(pz) - double(qz) : 0.0;
             });
-        else if (!kDraft && special <= 4)
+        else if (kDraft && tries <= 3) {                     // max(max(max(p - q, 0) - S1 q, 0) - S2 q, 0)
+            const double m1 = sm.mass[1], m2 = tries == 3 ? sm.mass[2] : 0.0;
+            sweep([&](int, float pj, float qj) {
+                const float pz = fmaxf(pj, 0.0f), qz = fmaxf(qj, 0.0f);
+                if (pz <= qz) return 0.0;
+                const double q = double(qz), r = double(pz) - q - m1 * q, r2 = r - m2 * q;
+                return r2 > 0.0 ? r2 : 0.0;                  // (what falls below 0 once stays there: all that follows is subtracted)
+            });
+        } else if (!kDraft && special <= 4)
             sweep([&](int j, float pj, float) {
                 return positive(j == gone[0] || j == gone[1] || j == gone[2] || j == gone[3] ? 0.0f : pj);
             });
