@@ -23,12 +23,16 @@
 
 namespace tl {
 
+struct SmallYes { static constexpr bool value = true; };
+struct SmallNo { static constexpr bool value = false; };
+
 template <int kDim, int kFmt, int kMT>
 struct SmallShape {
     static constexpr bool kBf16 = kFmt == TL_KV_BF16;
     static constexpr int kItem = kBf16 ? 2 : 1;
     static constexpr int kRowBytes = kDim * kItem;
-    static constexpr int kWarps = kDim == 256 ? 4 : 8;
+    static constexpr int kCtasPerSm = kMT == 1 && kRowBytes == 128 ? 3 : kMT == 1 && kRowBytes < 128 ? 2 : 1;
+    static constexpr int kWarps = kDim == 256 || kCtasPerSm == 3 ? 4 : 8;
     static constexpr int kThreads = kWarps * 32;
     static constexpr int kRows = kMT * 16;
     static constexpr int kTile = kWarps * 16;
@@ -38,18 +42,19 @@ struct SmallShape {
     static constexpr int kVChunks = kRowBytes / 8 / kVBytes;       // pieces of a token per thread (8 threads a row)
     static constexpr int kNTiles = kDim / 8;                       // 8-wide column tiles of p v
     static constexpr int kStageBytes = 32 * kRowBytes + 128;       // one warp's 16 tokens, keys and values, and the scales
-    static constexpr int kCtasPerSm = (kMT == 1 && kRowBytes <= 128) ? 2 : 1;
+    static constexpr int kSub = kMT == 1 && kRowBytes <= 128 ? 2 : 1;   // sub-tiles a warp takes at a time
     static constexpr int kQBytes = kMT * kSteps * 512;
     static constexpr int kStatBytes = (kWarps * kRows * 2 + kRows * 4) * 4;
-    static constexpr int kBudget = (kCtasPerSm == 2 ? 112 : 225) * 1024 - kQBytes - kStatBytes;
+    static constexpr int kLimit = (kCtasPerSm == 3 ? 74 : kCtasPerSm == 2 ? 112 : 225) * 1024;
+    static constexpr int kBudget = kLimit - kQBytes - kStatBytes;
     static constexpr int kStagesFit = kBudget / (kWarps * kStageBytes);
     static constexpr int kStages = kStagesFit > 6 ? 6 : kStagesFit;
     static constexpr int kRing = kWarps * kStages * kStageBytes;
     static constexpr int kJoin = kWarps * kRows * kDim * 4;
     static constexpr int kUnion = kRing > kJoin ? kRing : kJoin;   // the ring's memory also serves the join
     static constexpr int kSmem = kUnion + kQBytes + kStatBytes;
-    static_assert(kStages >= 2, "no room for two stages");
-    static_assert(kSmem <= (kCtasPerSm == 2 ? 113 : 227) * 1024, "shared memory");
+    static_assert(kStages >= 2 * kSub, "no room for the stages ahead");
+    static_assert(kSmem <= kLimit, "shared memory");
 };
 
 template <int kDim, int kFmt, int kMT>
@@ -97,6 +102,9 @@ attend_kernel(const AttendParams p) {
         int pages = load_page(lane), pages_next = load_page(lane + 32);
         pages = checked(pages, lane);
         uint32_t bad_any = 0;
+        // (offsets within a sub-tile fit 32 bits: the host bounds the token stride)
+        const uint32_t ts = uint32_t(p.cache.token_stride);
+        const uint32_t k_off = uint32_t(g) * ts + uint32_t(t) * 16u, v_off = uint32_t(2 * t) * ts + uint32_t(g) * uint32_t(S::kVBytes);
         auto issue = [&](int i) {                                        // starts the copies of sub-tile i (whole warp, i upwards)
             if (i < count) {
                 if (i > 0 && (i & 31) == 0) {
@@ -108,30 +116,35 @@ attend_kernel(const AttendParams p) {
                 bad_any |= ok ? 0u : 1u;
                 const int pos = pos_first + i * S::kTile;
                 const int line = pos & pos_mask;
-                const int left = len - pos;
+                const int left = ok ? len - pos : 0;
                 const int64_t at = ok ? int64_t(page) * p.cache.page_stride + int64_t(line) * p.cache.token_stride : 0;
+                const char* const k_at = k_head + at;
+                const char* const v_at = v_head + at;
                 const uint32_t dst = ring + uint32_t((i % S::kStages) * S::kStageBytes);
+                auto copy = [&](auto whole) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int tok = g + 8 * h;
-                    const bool in = ok && tok < left;
-                    const char* src = in ? k_head + at + tok * p.cache.token_stride : k_head;
+                    for (int h = 0; h < 2; ++h) {
+                        const bool in = decltype(whole)::value || g + 8 * h < left;
+                        const char* src = in ? k_at + (k_off + uint32_t(8 * h) * ts) : k_head;
 #pragma unroll
-                    for (int c = 0; c < S::kKChunks; ++c)
-                        cp_async_16(dst + uint32_t((h * S::kKChunks + c) * 512 + lane * 16), src + c * 64 + t * 16, in);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int tok = 2 * t + (k & 1) + 8 * (k >> 1);
-                    const bool in = ok && tok < left;
-                    const char* src = in ? v_head + at + tok * p.cache.token_stride : v_head;
-#pragma unroll
-                    for (int c = 0; c < S::kVChunks; ++c) {
-                        const uint32_t to = dst + uint32_t(16 * S::kRowBytes + (k * S::kVChunks + c) * 32 * S::kVBytes + lane * S::kVBytes);
-                        if (S::kVBytes == 16) cp_async_16(to, src + c * 128 + g * 16, in);
-                        else cp_async_8(to, src + g * 8, in);
+                        for (int c = 0; c < S::kKChunks; ++c)
+                            cp_async_16(dst + uint32_t((h * S::kKChunks + c) * 512 + lane * 16), src + c * 64, in);
                     }
-                }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int more = (k & 1) + 8 * (k >> 1);
+                        const bool in = decltype(whole)::value || 2 * t + more < left;
+                        const char* src = in ? v_at + (v_off + uint32_t(more) * ts) : v_head;
+#pragma unroll
+                        for (int c = 0; c < S::kVChunks; ++c) {
+                            const uint32_t to = dst + uint32_t(16 * S::kRowBytes + (k * S::kVChunks + c) * 32 * S::kVBytes + lane * S::kVBytes);
+                            if (S::kVBytes == 16) cp_async_16(to, src + c * 128, in);
+                            else cp_async_8(to, src, in);
+                        }
+                    }
+                };
+                if (left >= 16) copy(SmallYes{});
+                else copy(SmallNo{});
                 if (!kBf16 && lane < 8) {
                     // (the scales of a page's 16 tokens are read whole; those past the end belong to masked positions)
                     const float* sc = p.cache.scale[lane >> 2] + (ok ? int64_t(page) * p.cache.scale_page_stride + int64_t(w.head) * p.cache.scale_head_stride + line : 0);
@@ -141,7 +154,7 @@ attend_kernel(const AttendParams p) {
             cp_async_commit();
         };
 #pragma unroll
-        for (int i = 0; i < S::kStages - 1; ++i) issue(i);
+        for (int i = 0; i < S::kStages - S::kSub; ++i) issue(i);
 
         // the query rows as A fragments: warp by warp, one row at a time
         for (int r = warp; r < S::kRows; r += S::kWarps) {
@@ -208,210 +221,261 @@ attend_kernel(const AttendParams p) {
             }
         }
 
-        for (int i = 0; i < count; ++i) {
-            cp_async_wait<S::kStages - 2>();
+        for (int i = 0; i < count; i += S::kSub) {
+            // stages i .. i + kSub - 1 have landed; the slots of the last turn are free
+            cp_async_wait<S::kStages - 2 * S::kSub>();
             __syncwarp();
-            issue(i + S::kStages - 1);
-            const char* const st = ring_gen + (i % S::kStages) * S::kStageBytes;
-            float s[kMT][2][4];
 #pragma unroll
-            for (int mt = 0; mt < kMT; ++mt)
+            for (int u = 0; u < S::kSub; ++u) issue(i + S::kStages - S::kSub + u);
+            const char* st[S::kSub];
+            bool here[S::kSub];                                        // (at an odd end the last turn has one sub-tile less)
+            float s[S::kSub][kMT][2][4];
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[mt][nt][e] = 0.0f;
-#pragma unroll
-            for (int c = 0; c < S::kKChunks; ++c) {
-                const uint4 k0 = *reinterpret_cast<const uint4*>(st + c * 512 + lane * 16);
-                const uint4 k1 = *reinterpret_cast<const uint4*>(st + (S::kKChunks + c) * 512 + lane * 16);
-                const uint32_t a0[4] = {k0.x, k0.y, k0.z, k0.w}, a1[4] = {k1.x, k1.y, k1.z, k1.w};
-                constexpr int kStepsPer = kBf16 ? 2 : 4;
-#pragma unroll
-                for (int q = 0; q < kStepsPer; ++q) {
-                    uint32_t b00, b01, b10, b11;
-                    if (kBf16) {
-                        b00 = a0[2 * q], b01 = a0[2 * q + 1];
-                        b10 = a1[2 * q], b11 = a1[2 * q + 1];
-                    } else {
-                        codes4_to_f16<kFmt>(a0[q], b00, b01);
-                        codes4_to_f16<kFmt>(a1[q], b10, b11);
-                    }
-#pragma unroll
-                    for (int mt = 0; mt < kMT; ++mt) {
-                        const uint4 f = q_frag[(mt * S::kSteps + c * kStepsPer + q) * 32 + lane];
-                        const uint32_t a[4] = {f.x, f.y, f.z, f.w};
-                        mma_16816<kBf16>(s[mt][0], a, b00, b01);
-                        mma_16816<kBf16>(s[mt][1], a, b10, b11);
-                    }
-                }
-            }
-            // scores in log2 units; thread's positions: nt * 8 + 2t + {0, 1}
-            const int pos0 = pos_first + i * S::kTile;
-            float rvs[2][2];
-            if (!kBf16) {
-                const float* sc = reinterpret_cast<const float*>(st + 32 * S::kRowBytes);
-#pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
-                    const float2 ks = *reinterpret_cast<const float2*>(sc + nt * 8 + 2 * t);
-                    const float2 vs = *reinterpret_cast<const float2*>(sc + 16 + nt * 8 + 2 * t);
-                    // A row of zero values has scale 0: a tiny one in its place gives it its share of the sum.  A NaN
-                    // scale reaches the score alone (the product with 0), which a mask can still replace.
-                    const float v0 = vs.x >= 1e-30f ? vs.x : 1e-30f, v1 = vs.y >= 1e-30f ? vs.y : 1e-30f;
-                    const float lv0 = fmaf(vs.x, 0.0f, lg2(v0)), lv1 = fmaf(vs.y, 0.0f, lg2(v1));
-                    rvs[nt][0] = __fdividef(1.0f, v0);
-                    rvs[nt][1] = __fdividef(1.0f, v1);
-#pragma unroll
-                    for (int mt = 0; mt < kMT; ++mt)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            s[mt][nt][2 * h] = fmaf(s[mt][nt][2 * h], fac[mt][h] * ks.x, lv0);
-                            s[mt][nt][2 * h + 1] = fmaf(s[mt][nt][2 * h + 1], fac[mt][h] * ks.y, lv1);
-                        }
-                }
-            } else {
-#pragma unroll
-                for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                    for (int mt = 0; mt < kMT; ++mt)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            s[mt][nt][2 * h] *= fac[mt][h];
-                            s[mt][nt][2 * h + 1] *= fac[mt][h];
-                        }
-            }
-            const bool edge = pos0 + 16 > start;                       // the step's own tokens, or past the end
-            uint32_t seen = 0xffffffffu;                               // bit ((mt * 2 + h) * 4 + nt * 2 + e)
-            if (edge || bad_any) {
-                seen = 0;
-                const int page = table[pos0 >> p.cache.page_shift];
-                const bool ok = page >= 0 && page < p.cache.pages;
+            for (int u = 0; u < S::kSub; ++u) {
+                here[u] = u == 0 || i + u < count;
+                st[u] = ring_gen + ((i + u) % S::kStages) * S::kStageBytes;
 #pragma unroll
                 for (int mt = 0; mt < kMT; ++mt)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                    for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int pos = pos0 + (e >> 1) * 8 + 2 * t + (e & 1);
-                            const bool vis = ok && pos < len && attend_sees(p, w.a.r.first + tok_of[mt][h], tok_of[mt][h], pos - start);
-                            if (vis) seen |= 1u << ((mt * 2 + h) * 4 + e);
-                            else s[mt][e >> 1][2 * h + (e & 1)] = -INFINITY;
-                        }
+                        for (int e = 0; e < 4; ++e) s[u][mt][nt][e] = 0.0f;
             }
-            uint32_t a[kMT][4], a_low[kMT][4];
-            float pf[kMT][2][4];
+#pragma unroll
+            for (int c = 0; c < S::kKChunks; ++c) {
+                constexpr int kStepsPer = kBf16 ? 2 : 4;
+                uint32_t a0[S::kSub][4], a1[S::kSub][4];
+#pragma unroll
+                for (int u = 0; u < S::kSub; ++u) {
+                    const uint4 k0 = *reinterpret_cast<const uint4*>(st[u] + c * 512 + lane * 16);
+                    const uint4 k1 = *reinterpret_cast<const uint4*>(st[u] + (S::kKChunks + c) * 512 + lane * 16);
+                    a0[u][0] = k0.x, a0[u][1] = k0.y, a0[u][2] = k0.z, a0[u][3] = k0.w;
+                    a1[u][0] = k1.x, a1[u][1] = k1.y, a1[u][2] = k1.z, a1[u][3] = k1.w;
+                }
+#pragma unroll
+                for (int q = 0; q < kStepsPer; ++q) {
+                    uint32_t f4[kMT][4];
+#pragma unroll
+                    for (int mt = 0; mt < kMT; ++mt) {
+                        const uint4 f = q_frag[(mt * S::kSteps + c * kStepsPer + q) * 32 + lane];
+                        f4[mt][0] = f.x, f4[mt][1] = f.y, f4[mt][2] = f.z, f4[mt][3] = f.w;
+                    }
+#pragma unroll
+                    for (int u = 0; u < S::kSub; ++u) {
+                        uint32_t b00, b01, b10, b11;
+                        if (kBf16) {
+                            b00 = a0[u][(2 * q) & 3], b01 = a0[u][(2 * q + 1) & 3];
+                            b10 = a1[u][(2 * q) & 3], b11 = a1[u][(2 * q + 1) & 3];
+                        } else {
+                            codes4_to_f16<kFmt>(a0[u][q & 3], b00, b01);
+                            codes4_to_f16<kFmt>(a1[u][q & 3], b10, b11);
+                        }
+#pragma unroll
+                        for (int mt = 0; mt < kMT; ++mt) {
+                            mma_16816<kBf16>(s[u][mt][0], f4[mt], b00, b01);
+                            mma_16816<kBf16>(s[u][mt][1], f4[mt], b10, b11);
+                        }
+                    }
+                }
+            }
+            // scores in log2 units; the thread's positions: nt * 8 + 2t + {0, 1} of each sub-tile
+            float rvs[S::kSub][2][2];
+            uint32_t seen[S::kSub];                                    // bit ((mt * 2 + h) * 4 + nt * 2 + e)
+            bool edge[S::kSub];
+#pragma unroll
+            for (int u = 0; u < S::kSub; ++u) {
+                if (!kBf16) {
+                    const float* sc = reinterpret_cast<const float*>(st[u] + 32 * S::kRowBytes);
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt) {
+                        const float2 ks = *reinterpret_cast<const float2*>(sc + nt * 8 + 2 * t);
+                        const float2 vs = *reinterpret_cast<const float2*>(sc + 16 + nt * 8 + 2 * t);
+                        // A row of zero values has scale 0: a tiny one in its place gives it its share of the sum.  A NaN
+                        // scale reaches the score alone (the product with 0), which a mask can still replace.
+                        const float v0 = vs.x >= 1e-30f ? vs.x : 1e-30f, v1 = vs.y >= 1e-30f ? vs.y : 1e-30f;
+                        const float lv0 = fmaf(vs.x, 0.0f, lg2(v0)), lv1 = fmaf(vs.y, 0.0f, lg2(v1));
+                        rvs[u][nt][0] = __fdividef(1.0f, v0);
+                        rvs[u][nt][1] = __fdividef(1.0f, v1);
+#pragma unroll
+                        for (int mt = 0; mt < kMT; ++mt)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                s[u][mt][nt][2 * h] = fmaf(s[u][mt][nt][2 * h], fac[mt][h] * ks.x, lv0);
+                                s[u][mt][nt][2 * h + 1] = fmaf(s[u][mt][nt][2 * h + 1], fac[mt][h] * ks.y, lv1);
+                            }
+                    }
+                } else {
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                        for (int mt = 0; mt < kMT; ++mt)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                s[u][mt][nt][2 * h] *= fac[mt][h];
+                                s[u][mt][nt][2 * h + 1] *= fac[mt][h];
+                            }
+                }
+                const int pos0 = pos_first + (i + u) * S::kTile;
+                edge[u] = pos0 + 16 > start;                           // the step's own tokens, or past the end
+                seen[u] = 0xffffffffu;
+                if (edge[u] || bad_any || !here[u]) {
+                    seen[u] = 0;
+                    bool ok = here[u];
+                    if (ok) {
+                        const int page = table[pos0 >> p.cache.page_shift];
+                        ok = page >= 0 && page < p.cache.pages;
+                    }
+#pragma unroll
+                    for (int mt = 0; mt < kMT; ++mt)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int pos = pos0 + (e >> 1) * 8 + 2 * t + (e & 1);
+                                const bool vis = ok && pos < len && attend_sees(p, w.a.r.first + tok_of[mt][h], tok_of[mt][h], pos - start);
+                                if (vis) seen[u] |= 1u << ((mt * 2 + h) * 4 + e);
+                                else s[u][mt][e >> 1][2 * h + (e & 1)] = -INFINITY;
+                            }
+                    if (!kBf16 && !here[u]) rvs[u][0][0] = rvs[u][0][1] = rvs[u][1][0] = rvs[u][1][1] = 0.0f;   // (never loaded)
+                }
+            }
+            // The maximum may lag by up to 2^8: weights are at most 256 then, which f16 and the sums have room for, and the
+            // rescaling of O, half of all turns with an exact maximum, becomes rare.
+            float top[kMT][2];
+            bool grew = false;
 #pragma unroll
             for (int mt = 0; mt < kMT; ++mt)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float top = fmaxf(fmaxf(s[mt][0][2 * h], s[mt][0][2 * h + 1]), fmaxf(s[mt][1][2 * h], s[mt][1][2 * h + 1]));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    const float m_new = fmaxf(m[mt][h], top);
-                    // (a row that has seen nothing yet has maximum -inf: any finite number serves in its place)
-                    const float m_use = m_new == -INFINITY ? 0.0f : m_new;
-                    const bool grew = m_new > m[mt][h];
-                    if (__any_sync(0xffffffffu, grew)) {
-                        const float f = ex2(m[mt][h] - m_use);
+                    float x = -INFINITY;
+#pragma unroll
+                    for (int u = 0; u < S::kSub; ++u)
+                        x = fmaxf(x, fmaxf(fmaxf(s[u][mt][0][2 * h], s[u][mt][0][2 * h + 1]), fmaxf(s[u][mt][1][2 * h], s[u][mt][1][2 * h + 1])));
+                    top[mt][h] = x;
+                    grew |= x > m[mt][h] + 8.0f;
+                }
+            if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+                for (int mt = 0; mt < kMT; ++mt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float x = fmaxf(top[mt][h], __shfl_xor_sync(0xffffffffu, top[mt][h], 1));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+                        const float m_new = fmaxf(m[mt][h], x);
+                        const float f = m_new == -INFINITY ? 1.0f : ex2(m[mt][h] - m_new);
+                        m[mt][h] = m_new;
                         l[mt][h] *= f;
 #pragma unroll
                         for (int j = 0; j < S::kNTiles; ++j) {
                             o[mt][j][2 * h] *= f;
                             o[mt][j][2 * h + 1] *= f;
                         }
-                        m[mt][h] = m_new;
                     }
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const float e2 = ex2(s[mt][nt][2 * h + e] - m_use);
-                            pf[mt][nt][2 * h + e] = e2;
-                            sum += kBf16 ? e2 : e2 * rvs[nt][e];
-                        }
-                    l[mt][h] += sum;
-#pragma unroll
-                    for (int nt = 0; nt < 2; ++nt) {
-                        const float lo = pf[mt][nt][2 * h], hi = pf[mt][nt][2 * h + 1];
-                        a[mt][nt * 2 + h] = kBf16 ? pack_bf16(lo, hi) : pack_f16(lo, hi);
-                        // what the rounding to bf16 left over
-                        if (kBf16) a_low[mt][nt * 2 + h] = pack_bf16(lo - __uint_as_float(a[mt][nt * 2 + h] << 16), hi - __uint_as_float(a[mt][nt * 2 + h] & 0xffff0000u));
-                    }
-                }
-            const char* const vst = st + 16 * S::kRowBytes;
-            if (kBf16 && edge) {
-                // A value may be infinite or NaN for a token that other rows see: its product with a masked weight of 0
-                // must not reach this row.  (8-bit codes are always finite, and positions past the end were filled with 0.)
-                bool odd = false;
-#pragma unroll
-                for (int k = 0; k < 4 * S::kVChunks; ++k) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(vst + k * 512 + lane * 16);
-                    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) odd |= (u[q] & 0x7f80u) == 0x7f80u || (u[q] & 0x7f800000u) == 0x7f800000u;
-                }
-                if (__any_sync(0xffffffffu, odd)) {
-                    for (int tok = 0; tok < 16; ++tok) {
-                        const int from = g * 4 + (tok % 8) / 2, k = (tok >> 3) * 2 + (tok & 1);
-#pragma unroll
-                        for (int mt = 0; mt < kMT; ++mt)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const float own0 = tok & 1 ? pf[mt][0][2 * h + 1] : pf[mt][0][2 * h];
-                                const float own1 = tok & 1 ? pf[mt][1][2 * h + 1] : pf[mt][1][2 * h];
-                                const float pw = __shfl_sync(0xffffffffu, tok >> 3 ? own1 : own0, from);
-                                const uint32_t vis = __shfl_sync(0xffffffffu, seen, from) >> ((mt * 2 + h) * 4 + (tok >> 3) * 2 + (tok & 1)) & 1u;
-                                if (!vis) continue;
-#pragma unroll
-                                for (int j = 0; j < S::kNTiles; ++j)
-#pragma unroll
-                                    for (int e = 0; e < 2; ++e) {
-                                        const char* v = vst + (k * S::kVChunks + j / 8) * 512 + ((2 * t + e) * 4 + (tok % 8) / 2) * 16 + (j % 8) * 2;
-                                        o[mt][j][2 * h + e] += pw * __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(v));
-                                    }
-                            }
-                    }
-                    continue;
-                }
             }
 #pragma unroll
-            for (int c = 0; c < S::kVChunks; ++c) {
-                constexpr int kWords = S::kVBytes / 4;
-                uint32_t v[4][kWords];
+            for (int u = 0; u < S::kSub; ++u) {
+                if (u > 0 && !here[u]) break;
+                uint32_t a[kMT][4], a_low[kMT][4];
+                float pf[kMT][2][4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const char* src = vst + (k * S::kVChunks + c) * 32 * S::kVBytes + lane * S::kVBytes;
-                    if (S::kVBytes == 16) {
-                        const uint4 u = *reinterpret_cast<const uint4*>(src);
-                        v[k][0] = u.x, v[k][1 % kWords] = u.y, v[k][2 % kWords] = u.z, v[k][3 % kWords] = u.w;
-                    } else {
-                        const uint2 u = *reinterpret_cast<const uint2*>(src);
-                        v[k][0] = u.x, v[k][1 % kWords] = u.y;
+                for (int mt = 0; mt < kMT; ++mt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        // (a row that has seen nothing yet has maximum -inf: any finite number serves in its place)
+                        const float m_use = m[mt][h] == -INFINITY ? 0.0f : m[mt][h];
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float e2 = ex2(s[u][mt][nt][2 * h + e] - m_use);
+                                pf[mt][nt][2 * h + e] = e2;
+                                sum = kBf16 ? sum + e2 : fmaf(e2, rvs[u][nt][e], sum);
+                            }
+                        l[mt][h] += sum;
+#pragma unroll
+                        for (int nt = 0; nt < 2; ++nt) {
+                            const float lo = pf[mt][nt][2 * h], hi = pf[mt][nt][2 * h + 1];
+                            a[mt][nt * 2 + h] = kBf16 ? pack_bf16(lo, hi) : pack_f16(lo, hi);
+                            // what the rounding to bf16 left over
+                            if (kBf16) a_low[mt][nt * 2 + h] = pack_bf16(lo - __uint_as_float(a[mt][nt * 2 + h] << 16), hi - __uint_as_float(a[mt][nt * 2 + h] & 0xffff0000u));
+                        }
+                    }
+                const char* const vst = st[u] + 16 * S::kRowBytes;
+                if (kBf16 && edge[u]) {
+                    // A value may be infinite or NaN for a token that other rows see: its product with a masked weight of 0
+                    // must not reach this row.  (8-bit codes are always finite, and positions past the end were filled with 0.)
+                    bool odd = false;
+#pragma unroll
+                    for (int k = 0; k < 4 * S::kVChunks; ++k) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(vst + k * 512 + lane * 16);
+                        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) odd |= (x[q] & 0x7f80u) == 0x7f80u || (x[q] & 0x7f800000u) == 0x7f800000u;
+                    }
+                    if (__any_sync(0xffffffffu, odd)) {
+                        for (int tok = 0; tok < 16; ++tok) {
+                            const int from = g * 4 + (tok % 8) / 2, k = (tok >> 3) * 2 + (tok & 1);
+#pragma unroll
+                            for (int mt = 0; mt < kMT; ++mt)
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {
+                                    const float own0 = tok & 1 ? pf[mt][0][2 * h + 1] : pf[mt][0][2 * h];
+                                    const float own1 = tok & 1 ? pf[mt][1][2 * h + 1] : pf[mt][1][2 * h];
+                                    const float pw = __shfl_sync(0xffffffffu, tok >> 3 ? own1 : own0, from);
+                                    const uint32_t vis = __shfl_sync(0xffffffffu, seen[u], from) >> ((mt * 2 + h) * 4 + (tok >> 3) * 2 + (tok & 1)) & 1u;
+                                    if (!vis) continue;
+#pragma unroll
+                                    for (int j = 0; j < S::kNTiles; ++j)
+#pragma unroll
+                                        for (int e = 0; e < 2; ++e) {
+                                            const char* v = vst + (k * S::kVChunks + j / 8) * 512 + ((2 * t + e) * 4 + (tok % 8) / 2) * 16 + (j % 8) * 2;
+                                            o[mt][j][2 * h + e] += pw * __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(v));
+                                        }
+                                }
+                        }
+                        continue;
                     }
                 }
 #pragma unroll
-                for (int q = 0; q < kWords; ++q) {
-                    if (kBf16) {
-                        const uint32_t b[4] = {__byte_perm(v[0][q], v[1][q], 0x5410), __byte_perm(v[2][q], v[3][q], 0x5410),
-                                               __byte_perm(v[0][q], v[1][q], 0x7632), __byte_perm(v[2][q], v[3][q], 0x7632)};
+                for (int c = 0; c < S::kVChunks; ++c) {
+                    constexpr int kWords = S::kVBytes / 4;
+                    uint32_t v[4][kWords];
 #pragma unroll
-                        for (int mt = 0; mt < kMT; ++mt) {
-                            mma_16816<true>(o[mt][(c * kWords + q) * 2], a[mt], b[0], b[1]);
-                            mma_16816<true>(o[mt][(c * kWords + q) * 2 + 1], a[mt], b[2], b[3]);
-                            mma_16816<true>(o[mt][(c * kWords + q) * 2], a_low[mt], b[0], b[1]);
-                            mma_16816<true>(o[mt][(c * kWords + q) * 2 + 1], a_low[mt], b[2], b[3]);
+                    for (int k = 0; k < 4; ++k) {
+                        const char* src = vst + (k * S::kVChunks + c) * 32 * S::kVBytes + lane * S::kVBytes;
+                        if (S::kVBytes == 16) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(src);
+                            v[k][0] = x.x, v[k][1 % kWords] = x.y, v[k][2 % kWords] = x.z, v[k][3 % kWords] = x.w;
+                        } else {
+                            const uint2 x = *reinterpret_cast<const uint2*>(src);
+                            v[k][0] = x.x, v[k][1 % kWords] = x.y;
                         }
-                    } else {
-                        uint32_t lo[4], hi[4];
-                        codes4_to_f16<kFmt>(__byte_perm(v[0][q], v[1][q], 0x5140), lo[0], lo[1]);
-                        codes4_to_f16<kFmt>(__byte_perm(v[0][q], v[1][q], 0x7362), lo[2], lo[3]);
-                        codes4_to_f16<kFmt>(__byte_perm(v[2][q], v[3][q], 0x5140), hi[0], hi[1]);
-                        codes4_to_f16<kFmt>(__byte_perm(v[2][q], v[3][q], 0x7362), hi[2], hi[3]);
+                    }
 #pragma unroll
-                        for (int z = 0; z < 4; ++z)
+                    for (int q = 0; q < kWords; ++q) {
+                        if (kBf16) {
+                            const uint32_t b[4] = {__byte_perm(v[0][q], v[1][q], 0x5410), __byte_perm(v[2][q], v[3][q], 0x5410),
+                                                   __byte_perm(v[0][q], v[1][q], 0x7632), __byte_perm(v[2][q], v[3][q], 0x7632)};
 #pragma unroll
-                            for (int mt = 0; mt < kMT; ++mt)
-                                mma_16816<false>(o[mt][(c * kWords + q) * 4 + z], a[mt], lo[z], hi[z]);
+                            for (int mt = 0; mt < kMT; ++mt) {
+                                mma_16816<true>(o[mt][(c * kWords + q) * 2], a[mt], b[0], b[1]);
+                                mma_16816<true>(o[mt][(c * kWords + q) * 2 + 1], a[mt], b[2], b[3]);
+                                mma_16816<true>(o[mt][(c * kWords + q) * 2], a_low[mt], b[0], b[1]);
+                                mma_16816<true>(o[mt][(c * kWords + q) * 2 + 1], a_low[mt], b[2], b[3]);
+                            }
+                        } else {
+                            uint32_t lo[4], hi[4];
+                            codes4_to_f16<kFmt>(__byte_perm(v[0][q], v[1][q], 0x5140), lo[0], lo[1]);
+                            codes4_to_f16<kFmt>(__byte_perm(v[0][q], v[1][q], 0x7362), lo[2], lo[3]);
+                            codes4_to_f16<kFmt>(__byte_perm(v[2][q], v[3][q], 0x5140), hi[0], hi[1]);
+                            codes4_to_f16<kFmt>(__byte_perm(v[2][q], v[3][q], 0x7362), hi[2], hi[3]);
+#pragma unroll
+                            for (int z = 0; z < 4; ++z)
+#pragma unroll
+                                for (int mt = 0; mt < kMT; ++mt)
+                                    mma_16816<false>(o[mt][(c * kWords + q) * 4 + z], a[mt], lo[z], hi[z]);
+                        }
                     }
                 }
             }

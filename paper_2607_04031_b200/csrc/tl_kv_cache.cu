@@ -30,6 +30,7 @@ int kv_view(const tl_kv_cache* c, KvView* out) {
     // (one head, or one page, makes the stride over it meaningless, but it still has to be a legal one)
     if (page <= 0 || head <= 0 || token < c->head_dim || spage <= 0 || shead <= 0) return TL_ERR_INVALID_ARG;
     if ((page * s) % 16 || (head * s) % 16 || (token * s) % 16) return TL_ERR_ALIGNMENT;
+    if (token * s > (int64_t(1) << 26)) return TL_ERR_UNSUPPORTED;      // sixteen tokens' offsets fit 32 bits
     if (reinterpret_cast<uintptr_t>(c->k) % 16 || reinterpret_cast<uintptr_t>(c->v) % 16) return TL_ERR_ALIGNMENT;
     if (c->format != TL_KV_BF16) {
         if (spage % 4 || shead % 4) return TL_ERR_ALIGNMENT;
