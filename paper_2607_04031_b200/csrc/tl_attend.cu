@@ -14,11 +14,9 @@ __global__ void __launch_bounds__(kCombineThreads) attend_combine_kernel(const A
     pdl_launch_dependents();
     // (The lengths may be read ahead of the wait: every CTA of the attention kernel has let this one start after its own
     // wait, so whatever wrote them is over.)
-    const int total = attend_total(p), per = attend_per_cta(total, p.ctas);
-    const int64_t border64 = (int64_t(blockIdx.x) + 1) * per;
-    if (border64 >= total) return;
-    const int border = int(border64);
-    const AttendPlace w = attend_locate(p, border);
+    int per, border, border_end;
+    AttendPlace w;
+    if (!attend_range(p, int(blockIdx.x) + 1, &per, &border, &border_end, &w)) return;
     if (w.tile == 0) return;                                  // the border lies between two units
     const int u0 = border - w.tile, u1 = u0 + w.a.tiles;
     const int c0 = int(uint32_t(u0) / uint32_t(per)), c1 = int(uint32_t(u1 - 1) / uint32_t(per));

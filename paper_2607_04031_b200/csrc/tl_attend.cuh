@@ -45,20 +45,6 @@ __device__ __forceinline__ AttendRequest attend_request(const AttendParams& p, i
     a.tiles = (a.r.len + (1 << p.tile_shift) - 1) >> p.tile_shift;
     return a;
 }
-__device__ __forceinline__ int attend_request_tiles(const AttendParams& p, int b) {
-    if (b >= p.batch.requests) return 0;
-    const AttendRequest a = attend_request(p, b);
-    return a.tiles * a.row_blocks * p.cache.heads;
-}
-
-// Whole warp: the line's length (the host refuses batches that could have 2^31 tiles or more).
-__device__ __forceinline__ int attend_total(const AttendParams& p) {
-    int sum = 0;
-    for (int b = int(lane_id()); b < p.batch.requests; b += 32) sum += attend_request_tiles(p, b);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    return sum;
-}
 __device__ __forceinline__ int attend_per_cta(int total, int ctas) { return int(uint32_t(total + ctas - 1) / uint32_t(ctas)); }
 
 struct AttendPlace {
@@ -66,33 +52,63 @@ struct AttendPlace {
     int tile;
     AttendRequest a;
 };
-// Whole warp: where tile x of the line (x < total) lies.
-__device__ __forceinline__ AttendPlace attend_locate(const AttendParams& p, int x) {
-    AttendPlace w;
-    int before = 0;
+// Whole warp: the tiles of CTA `cta` are [*x, *x_end) of the line; w: where tile *x lies.  False: there are none.  (The host refuses batches that could have 2^31 tiles or more.)
+__device__ __forceinline__ bool attend_range(const AttendParams& p, int cta, int* per_out, int* x, int* x_end, AttendPlace* w) {
+    const int lane = int(lane_id());
+    // the requests' tiles, 32 at a time; a batch of up to 32 is looked at once, each lane keeping its request
+    AttendRequest mine;
+    int tiles = 0, total = 0;
+    for (int b = lane; b - lane < p.batch.requests; b += 32) {
+        tiles = 0;
+        if (b < p.batch.requests) {
+            mine = attend_request(p, b);
+            tiles = mine.tiles * mine.row_blocks * p.cache.heads;
+        }
+        total += tiles;
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    const int per = attend_per_cta(total, p.ctas);
+    const int64_t at = int64_t(cta) * per;
+    *per_out = per;
+    if (at >= total) return false;
+    *x = int(at);
+    *x_end = *x + min(per, total - *x);
+    int before = 0, owner = 0;
     for (int b0 = 0;; b0 += 32) {
-        const int mine = attend_request_tiles(p, b0 + int(lane_id()));
-        int run = mine;
+        if (p.batch.requests > 32) {
+            tiles = 0;
+            if (b0 + lane < p.batch.requests) {
+                mine = attend_request(p, b0 + lane);
+                tiles = mine.tiles * mine.row_blocks * p.cache.heads;
+            }
+        }
+        int run = tiles;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int up = __shfl_up_sync(0xffffffffu, run, d);
-            if (int(lane_id()) >= d) run += up;
+            if (lane >= d) run += up;
         }
-        const uint32_t past = __ballot_sync(0xffffffffu, before + run > x);
+        const uint32_t past = __ballot_sync(0xffffffffu, before + run > *x);
         if (past) {
-            const int l = __ffs(int(past)) - 1;
-            w.b = b0 + l;
-            before += __shfl_sync(0xffffffffu, run - mine, l);
+            owner = __ffs(int(past)) - 1;
+            w->b = b0 + owner;
+            before += __shfl_sync(0xffffffffu, run - tiles, owner);
             break;
         }
         before += __shfl_sync(0xffffffffu, run, 31);
     }
-    w.a = attend_request(p, w.b);
-    const uint32_t y = uint32_t(x - before), unit = y / uint32_t(w.a.tiles), head = unit / uint32_t(w.a.row_blocks);
-    w.tile = int(y - unit * uint32_t(w.a.tiles));
-    w.head = int(head);
-    w.block = int(unit - head * uint32_t(w.a.row_blocks));
-    return w;
+    w->a.r.first = __shfl_sync(0xffffffffu, mine.r.first, owner);
+    w->a.r.n = __shfl_sync(0xffffffffu, mine.r.n, owner);
+    w->a.r.start = __shfl_sync(0xffffffffu, mine.r.start, owner);
+    w->a.r.len = __shfl_sync(0xffffffffu, mine.r.len, owner);
+    w->a.row_blocks = __shfl_sync(0xffffffffu, mine.row_blocks, owner);
+    w->a.tiles = __shfl_sync(0xffffffffu, mine.tiles, owner);
+    const uint32_t y = uint32_t(*x - before), unit = y / uint32_t(w->a.tiles), head = unit / uint32_t(w->a.row_blocks);
+    w->tile = int(y - unit * uint32_t(w->a.tiles));
+    w->head = int(head);
+    w->block = int(unit - head * uint32_t(w->a.row_blocks));
+    return true;
 }
 // The first tile of the next unit; the caller knows that there is one.
 __device__ __forceinline__ void attend_next_unit(const AttendParams& p, AttendPlace& w) {

@@ -76,11 +76,10 @@ attend_kernel(const AttendParams p) {
 
     pdl_wait();
     pdl_launch_dependents();
-    const int total = attend_total(p), per = attend_per_cta(total, p.ctas);
-    int x = int(min(int64_t(blockIdx.x) * per, int64_t(total)));
-    const int x_end = x + min(per, total - x);
-    if (x >= x_end) return;
-    AttendPlace w = attend_locate(p, x);
+    int per, x = 0, x_end = 0;
+    AttendPlace w;
+    const bool work = attend_range(p, int(blockIdx.x), &per, &x, &x_end, &w);
+    if (!work) return;
 
     while (true) {
         const int t0 = w.tile, t1 = min(w.a.tiles, t0 + (x_end - x));

@@ -199,9 +199,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
 
     pdl_wait();
     pdl_launch_dependents();
-    const int total = attend_total(p), per = attend_per_cta(total, p.ctas);
-    int x0 = int(min(int64_t(blockIdx.x) * per, int64_t(total)));
-    const int x_end = x0 + min(per, total - x0);
+    int per, x0 = 0, x_end = 0;
+    AttendPlace w;
+    const bool work = attend_range(p, int(blockIdx.x), &per, &x0, &x_end, &w);
 
     auto wait = [&](uint64_t* bar, uint32_t parity) {
         return mbar_wait_bounded(bar, parity, abort_ptr, p.status, kWaitAttend, tp.wait_ns);
@@ -218,8 +218,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
         if (warp == kTcMmaWarp) tmem_dealloc(tmem, 512);
     };
 
-    if (x0 < x_end) {
-        AttendPlace w = attend_locate(p, x0);
+    if (work) {
         uint32_t tiles_before = 0;                             // tiles of this CTA's earlier units: ring positions count on
         uint32_t unit = 0;
         bool alive = true;
@@ -242,28 +241,30 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 const bool active = kBlocks == 2 ? stream * 128 < unit_rows : stream < tiles;
                 float fac = p.scale_log2;
                 {
-                    // this row of q, converted, into the operand tile (twice over the row: the scale first)
+                    // this row of q, converted, into the operand tile (all of the row's loads in flight at once)
+                    uint4 q[kDim / 8];
                     const uint4* src = reinterpret_cast<const uint4*>(p.q + int64_t(w.a.r.first + tok) * p.q_stride + int64_t(hq) * kDim);
+#pragma unroll
+                    for (int c = 0; c < kDim / 8; ++c) q[c] = __ldg(src + c);
                     float mul = 1.0f;
                     if (!kBf16) {
                         uint32_t top = 0;
-#pragma unroll 4
-                        for (int c = 0; c < kDim / 8; ++c) {
-                            const uint4 q = __ldg(src + c);
-                            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) top = max(top, max((u[i] << 16) & 0x7fff0000u, u[i] & 0x7fff0000u));
+                        for (int c = 0; c < kDim / 8; ++c) {
+                            const uint32_t u[4] = {q[c].x, q[c].y, q[c].z, q[c].w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) top = __vmaxu2(top, u[i] & 0x7fff7fffu);       // two bf16 patterns at a time
                         }
-                        const int e = int(top >> 23);
+                        const int e = int(max(top & 0xffffu, top >> 16) >> 7);
                         const int up = e == 0 || e == 255 ? 0 : min(127 + 14 - e, 100);
                         mul = __uint_as_float(uint32_t(127 + up) << 23);
                         fac *= __uint_as_float(uint32_t(127 - up) << 23);
                     }
                     if (kBlocks == 2 || stream == 0) {
                         char* const dst = smem + (kBlocks == 2 ? stream * S::kOperand : 0) + r * 128;
-#pragma unroll 4
+#pragma unroll
                         for (int c = 0; c < kDim / 8; ++c) {
-                            uint4 v = __ldg(src + c);
+                            uint4 v = q[c];
                             if (!kBf16) {
                                 uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
