@@ -110,11 +110,14 @@ typedef enum {
                                 4 = the next grouped launch builds the tile tables it prepares ahead of its stream
                                 predecessor's completion from wrong expert offsets, so that its check after the wait
                                 must find them wrong and build them again; the output is the ordinary one.
+                                5 = in the next tl_tree_attention launch that runs on tcgen05 (more than 32 query rows per
+                                key/value head on average) CTA 0 never announces its first key tile, so that the waits for it
+                                run out (detail 0xc00) and the CTA gives up; the rows it owns are undefined.
                                 The option resets itself to 0 when it is consumed. */
     TL_OPT_MOE_ROW_CAP,      /* grouped products: most token rows per tile; 0 (default): the library's choice (32, or 64 / 128 when
                                 the experts average more than 24 / 48 rows and there are enough such tiles), else 16/32/64/128 */
     TL_OPT_REDUCE_SPLIT,     /* 1 (default): a split tile's partial sums are added by all reduction CTAs inside it, 0: by one */
-    TL_OPT_SM_LIMIT,         /* 0 (default): GEMM grids use every SM; n > 0: at most n CTAs (leaves SMs to concurrent work) */
+    TL_OPT_SM_LIMIT,         /* 0 (default): GEMM and tree attention grids use every SM; n > 0: at most n SMs' CTAs (leaves SMs to concurrent work) */
     TL_OPT_NO_SCRATCH_PLANS, /* 1 (default): dense decode-sized products prefer schedules without partial tiles in global
                                 memory (whole tiles on a grid that divides the tile count, or split-K inside clusters);
                                 0: always the stream-K cut */
@@ -525,7 +528,7 @@ int tl_kv_read(const tl_kv_cache* cache, const tl_kv_batch* batch, void* d_k, vo
  * Moves the cache rows of the tokens that were kept: the row of position start[b] + accepted[b][i] goes to position
  * start[b] + i, for i < n_accepted[b].  accepted: device [requests][accepted_stride], increasing within a request
  * (what tl_tree_verify writes).  new_start (may be NULL, may be batch->start itself): device [requests], receives
- * start + n_accepted.  An index outside the request's rows, or below i, is skipped and reported (detail 0xB00).
+ * start + n_accepted.  An index outside the request's rows, or below i, is skipped and reported (detail 0xb00).
  * Codes and scales move as they are.  Asynchronous.
  */
 int tl_kv_commit(const tl_kv_cache* cache, const tl_kv_batch* batch, const int32_t* d_accepted, int64_t accepted_stride,

@@ -224,7 +224,7 @@ int tl_set_option(int option, int64_t value) {
         case TL_OPT_PREFETCH_STAGES: if (value < -1 || value > 16) return TL_ERR_INVALID_ARG; break;
         case TL_OPT_MAX_STAGES: if (value != 0 && (value < 2 || value > 16)) return TL_ERR_INVALID_ARG; break;
         case TL_OPT_WAIT_LIMIT_US: if (value < 100 || value > 60000000) return TL_ERR_INVALID_ARG; break;
-        case TL_OPT_STALL_ONCE: if (value < 0 || value > 4) return TL_ERR_INVALID_ARG; break;
+        case TL_OPT_STALL_ONCE: if (value < 0 || value > 5) return TL_ERR_INVALID_ARG; break;
         case TL_OPT_SM_LIMIT: if (value < 0 || value > 4096) return TL_ERR_INVALID_ARG; break;
         case TL_OPT_PLAN_AS_IF_SMS: if (value < 0 || value > 4096) return TL_ERR_INVALID_ARG; break;
         case TL_OPT_MOE_ROW_CAP: if (value != 0 && value != 16 && value != 32 && value != 64 && value != 128) return TL_ERR_INVALID_ARG; break;

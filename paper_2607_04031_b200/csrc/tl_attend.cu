@@ -81,6 +81,7 @@ static int attend_plan(const tl_kv_cache* cache, const tl_kv_batch* batch, int q
     const int64_t units = (ceil_div(int64_t(batch->tokens) * group, plan->mma_rows) + batch->requests) * cache->heads;
     if (double(tiles) * double(units) >= double(INT32_MAX)) return TL_ERR_UNSUPPORTED;
     int64_t ctas = int64_t(dev().sm_count) * plan->ctas_per_sm;
+    if (opt(TL_OPT_SM_LIMIT) > 0) ctas = std::min(ctas, opt(TL_OPT_SM_LIMIT) * plan->ctas_per_sm);
     if (tiles < ctas && units < ctas) ctas = std::min(ctas, tiles * units);
     plan->ctas = int(ctas);
     const bool split = plan->ctas > 1 && tiles > 1;

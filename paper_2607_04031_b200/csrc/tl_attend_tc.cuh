@@ -37,6 +37,7 @@ struct AttendTcParams {
     AttendParams a;
     CUtensorMap map[2];                  // keys, values (bf16 caches)
     int box_tokens;
+    int stall;                           // test hook: CTA 0's first key tile is never announced
     uint64_t wait_ns;
 };
 
@@ -300,6 +301,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     return lane & 16 ? r2 : r0;
                 };
                 bool odd = false;
+                // A stream without rows or tiles here keeps step with the other: ahead by two units, its arrivals alone would
+                // complete the barrier for queries that are not in place.
+                if (!active) {
+                    alive = warp_wait(&bars.q_full, unit & 1u);
+                    if (!alive) break;
+                }
                 const int step = kBlocks == 2 ? 1 : 2;
                 for (int n = kBlocks == 2 ? 0 : stream; active && n < tiles; n += step) {
                     const bool first = n < step;
@@ -676,7 +683,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             store(0, smem + S::kOffK + ki * S::kOperand);
                             fence_proxy_async_smem();
                             __syncwarp();
-                            if (lane == 0) mbar_arrive(&bars.k_full[ki]);
+                            if (lane == 0 && !(tp.stall && blockIdx.x == 0 && pt == 0 && at == 0)) mbar_arrive(&bars.k_full[ki]);
                         }
                         if (more) {
                             turn_to(n + 1);
@@ -769,7 +776,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             if (which && pt == 0 && !plain) bars.meta[vi] = bad;
                             if (which && lane == 0 && !(plain && pt == 0)) bars.odd[vi][warp - kTcProducerWarp] = any_odd;
                             __syncwarp();
-                            if (lane == 0 && !(plain && pt == 0)) mbar_arrive(full);
+                            if (lane == 0 && !(plain && pt == 0) && !(tp.stall && blockIdx.x == 0 && pt == 32 && at == 0 && which == 0)) mbar_arrive(full);
                         }
                         if (!alive) break;
                     }
@@ -782,6 +789,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 attend_next_unit(p, w);
             }
             if (bad_any && pt == 0) atomicCAS(p.status, 0u, kBadPage);
+            if (!kBf16) cp_async_wait<0>();
             if (kBf16 && !alive) {                             // gave up: wait (with a limit) for the copies in flight
                 const uint64_t since = global_timer_ns();
                 while (global_timer_ns() - since < 2000000ull) {}

@@ -15,6 +15,10 @@ int launch_attend_tc(const tl_kv_cache* cache, const AttendParams& p, cudaStream
     memset(&tp, 0, sizeof tp);
     tp.a = p;
     tp.wait_ns = wait_limit_ns();
+    if (opt(TL_OPT_STALL_ONCE) == 5) {
+        tp.stall = 1;
+        tl_set_option(TL_OPT_STALL_ONCE, 0);
+    }
     tp.box_tokens = std::min(cache->page_tokens, kTcTile);
     if (kFmt == TL_KV_BF16) {
         // [page][head][token][dim]; a box holds 64 dimensions (128 bytes, the swizzle's width) of one page's tokens

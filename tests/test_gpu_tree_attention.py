@@ -282,3 +282,96 @@ def test_pages_past_32_bit_offsets():
     kk, vv = (ref.held(*ref.quantise(t, "int8")) for t in (x, y))
     want, _, mass, big = ref.attention(q, kk, vv, n - 4, torch.ones(4, 4, dtype=torch.bool).tril(), dim ** -0.5)
     assert bool(((out.double().cpu() - want).abs() <= ref.attention_bound(want, mass, big, vv, "int8", dim, dim ** -0.5, n)).all())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads,group,counts", [(1, 8, [16, 5, 12, 0, 16]), (2, 8, [17, 40, 33]), (1, 4, [70, 1, 64]), (1, 16, [20, 9])])
+def test_many_rows_in_blocks(fmt, dim, heads, group, counts):
+    # 40 to 640 rows a request: one block of 128, one of 256 of which half or a few rows are used, several blocks
+    ctx = [130 * b + 61 for b in range(len(counts))]
+    Step(fmt, heads, group, dim, 16, ctx, counts, seed=dim + group + len(counts)).check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("most", [1, 12])
+def test_more_requests_than_a_warp_looks_at_at_once(fmt, most):
+    counts = [(5 * b) % (most + 1) for b in range(75)]
+    Step(fmt, 2, 4, 64, 16, [(31 * b) % 200 for b in range(75)], counts, trees="causal", seed=8).check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("counts", [[2], [50]])
+@pytest.mark.parametrize("step", [0.4, 3.0, 40.0])
+def test_a_maximum_that_grows_along_the_sequence(fmt, counts, step):
+    # every 16 positions the scores rise by a little, or by much, so that the running maximum is taken anew within tiles
+    # and between them
+    s = Step(fmt, 1, 4, 128, 16, [620], counts, seed=17)
+    g = torch.Generator().manual_seed(5)
+    direction = torch.randn(1, 1, 128, generator=g)
+    s.q[:] = (direction * 128 ** 0.5 / direction.norm() + 0.1 * torch.randn(s.q.shape, generator=g)).to(torch.bfloat16)
+    n = 620 + counts[0]
+    pos = torch.arange(n)
+    k = direction * (step * (pos // 16).float()).view(-1, 1, 1) / direction.norm() + 0.1 * torch.randn(n, 1, 128, generator=g)
+    s.pool.write(0, pos, k, torch.randn(n, 1, 128, generator=g))
+    s.check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("counts", [[3], [40]])
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 1.7])
+def test_any_scale(fmt, counts, scale):
+    from paper_2607_04031_b200 import binding as tl
+    s = Step(fmt, 2, 4, 128, 32, [300], counts, seed=23)
+    s.scale = scale
+    out = s.run()
+    tl.device_status()
+    if scale < 0:
+        # (q . k) * scale = (-q . k) * -scale: the bounds of the comparison are stated for scales that are not negative
+        s.q, s.scale = -s.q, -scale
+    s.compare(out.double().cpu(), s.lse.double().cpu())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(fmt):
+    from paper_2607_04031_b200 import binding as tl
+    s = Step(fmt, 2, 4, 128, 16, [500], [40], seed=3)
+    s.check()
+    with tl.option(tl.OPT_WAIT_LIMIT_US, 20000):
+        tl.set_option(tl.OPT_STALL_ONCE, 5)
+        s.run()
+        with pytest.raises(tl.TileLensError, match="c00"):
+            tl.device_status()
+    assert tl.get_option(tl.OPT_STALL_ONCE) == 0
+    s.check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("small,large", [(4, 90), (16, 60)])
+@pytest.mark.parametrize("sms", [1, 2])
+def test_many_small_units_among_large_ones(fmt, dim, small, large, sms):
+    # blocks of 256 rows by the average; most units have at most 128, several in a row in every CTA
+    from paper_2607_04031_b200 import binding as tl
+    counts = [small if b % 6 else large for b in range(1, 13)]
+    with tl.option(tl.OPT_SM_LIMIT, sms):
+        Step(fmt, 2, 8, dim, 16, [(29 * b) % 110 for b in range(12)], counts, trees="causal", seed=small + dim).check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("sms", [1, 2])
+def test_units_of_one_tile_among_longer_ones(fmt, dim, sms):
+    # blocks of 128 rows; the second stream has no tile in most units, several in a row in every CTA
+    from paper_2607_04031_b200 import binding as tl
+    with tl.option(tl.OPT_SM_LIMIT, sms):
+        Step(fmt, 2, 8, dim, 16, [(29 * b) % 110 if b % 5 else 300 for b in range(15)], [5 + b % 3 for b in range(15)], seed=dim).check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dim", [64, 256])
+@pytest.mark.parametrize("sms", [1, 3])
+def test_few_rows_on_few_multiprocessors(fmt, dim, sms):
+    from paper_2607_04031_b200 import binding as tl
+    with tl.option(tl.OPT_SM_LIMIT, sms):
+        Step(fmt, 2, 4, dim, 16, [(61 * b) % 230 for b in range(20)], [1 + b % 3 for b in range(20)], seed=dim).check()
