@@ -16,8 +16,12 @@ __global__ void __launch_bounds__(kCombineThreads) attend_combine_kernel(const A
     // wait, so whatever wrote them is over.)
     int per, border, border_end;
     AttendPlace w;
-    if (!attend_range(p, int(blockIdx.x) + 1, &per, &border, &border_end, &w)) return;
-    if (w.tile == 0) return;                                  // the border lies between two units
+    if (!attend_range(p, int(blockIdx.x) + 1, &per, &border, &border_end, &w) || w.tile == 0) {
+        // Nothing to join: the line ends ahead of the border, or the border lies between two units.  One block waits all the
+        // same: what follows waits for this grid alone, which must not be over before the attention kernel is.
+        if (blockIdx.x == 0 && blockIdx.y == 0) pdl_wait();
+        return;
+    }
     const int u0 = border - w.tile, u1 = u0 + w.a.tiles;
     const int c0 = int(uint32_t(u0) / uint32_t(per)), c1 = int(uint32_t(u1 - 1) / uint32_t(per));
     const int share = (int(blockIdx.x) - c0) * int(gridDim.y) + int(blockIdx.y), shares = (c1 - c0) * int(gridDim.y);
