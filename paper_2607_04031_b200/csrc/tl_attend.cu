@@ -68,24 +68,39 @@ static auto attend_tc_of(int format) {
     return format == TL_KV_BF16 ? attend_tc_bf16 : format == TL_KV_E4M3 ? attend_tc_e4m3 : attend_tc_int8;
 }
 
-// Which kernel a call runs, from what the host knows: the query rows per key/value head of an average request.
+// Which kernel a call runs, from what the host knows: the query rows per key/value head of an average request, and the
+// most tiles there can be.  Measured with 64 query and 8 key/value heads over 4100 positions (2000 with 64 requests):
+//   few-row kernel or tcgen05, us:   head_dim 128    24 rows: 16 requests bf16 81 / 87, 64 requests INT8 89 / 128,
+//                                                    4 requests INT8 34 / 28
+//                                                    32 rows: 16 requests bf16 87 / 87, E4M3 77 / 71, 64 requests INT8 144 / 130
+//                                    head_dim 64     32 rows: 16 requests bf16 60 / 69, E4M3 48 / 60; one request equal
+//                                    (either)        64 rows: 16 requests bf16 146 / 93, E4M3 126 / 77
+//   blocks of 128 or 256 rows, us:   256 rows: 1 request bf16 42 / 54, 4 requests E4M3 56 / 63 (7 tiles per SM),
+//                                    8 requests bf16 95 / 85 (14 tiles per SM), 8 over 8000 140 / 118
+//                                    160 rows: 8 over 8000 E4M3 97 / 108; 192 rows: 110 / 110
+// Blocks of 256 fetch and convert every tile for two streams at once, but need rows to fill them and more than a few
+// tiles per SM to pay for the wider joins.
+constexpr int kBlockRowsFrom = 192, kBlockTilesFrom = 10;
 static int attend_plan(const tl_kv_cache* cache, const tl_kv_batch* batch, int q_heads, AttendPlan* plan) {
     const int group = q_heads / cache->heads;
     const int64_t rows = ceil_div(batch->tokens, batch->requests) * group;
-    if (rows > 32 && cache->head_dim <= 128) {
-        plan->mma_rows = rows > 128 ? 256 : 128;
+    const int64_t room = std::min(batch->table_stride * cache->page_tokens, kKvMaxTokens);
+    int64_t sms = dev().sm_count;
+    if (opt(TL_OPT_SM_LIMIT) > 0) sms = std::min(sms, opt(TL_OPT_SM_LIMIT));
+    if (cache->head_dim <= 128 && rows > (cache->head_dim == 128 ? 24 : 32)) {
         plan->tile_tokens = 128;
         plan->ctas_per_sm = 1;
+        const double tiles256 = double(batch->requests) * cache->heads * double(ceil_div(rows, 256)) * double(ceil_div(room, 128));
+        plan->mma_rows = rows >= kBlockRowsFrom && tiles256 >= double(kBlockTilesFrom * sms) ? 256 : 128;
     } else {
         plan->mma_rows = rows > 16 && cache->head_dim <= 128 ? 32 : 16;
         if (int rc = attend_small_of(cache->format)(false, cache->head_dim, plan->mma_rows, &plan->tile_tokens, &plan->ctas_per_sm, nullptr, 0, nullptr)) return rc;
     }
     // no more CTAs than there can be tiles (the length is bounded by the page table)
-    const int64_t tiles = ceil_div(std::min(batch->table_stride * cache->page_tokens, kKvMaxTokens), plan->tile_tokens);
+    const int64_t tiles = ceil_div(room, plan->tile_tokens);
     const int64_t units = (ceil_div(int64_t(batch->tokens) * group, plan->mma_rows) + batch->requests) * cache->heads;
     if (double(tiles) * double(units) >= double(INT32_MAX)) return TL_ERR_UNSUPPORTED;
-    int64_t ctas = int64_t(dev().sm_count) * plan->ctas_per_sm;
-    if (opt(TL_OPT_SM_LIMIT) > 0) ctas = std::min(ctas, opt(TL_OPT_SM_LIMIT) * plan->ctas_per_sm);
+    int64_t ctas = sms * plan->ctas_per_sm;
     if (tiles < ctas && units < ctas) ctas = std::min(ctas, tiles * units);
     plan->ctas = int(ctas);
     const bool split = plan->ctas > 1 && tiles > 1;

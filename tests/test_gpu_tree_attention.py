@@ -348,7 +348,7 @@ def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(fmt):
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("dim", [64, 128])
-@pytest.mark.parametrize("small,large", [(4, 90), (16, 60)])
+@pytest.mark.parametrize("small,large", [(4, 90), (16, 60), (4, 150), (16, 110)])
 @pytest.mark.parametrize("sms", [1, 2])
 def test_many_small_units_among_large_ones(fmt, dim, small, large, sms):
     # blocks of 256 rows by the average; most units have at most 128, several in a row in every CTA
@@ -375,3 +375,66 @@ def test_few_rows_on_few_multiprocessors(fmt, dim, sms):
     from paper_2607_04031_b200 import binding as tl
     with tl.option(tl.OPT_SM_LIMIT, sms):
         Step(fmt, 2, 4, dim, 16, [(61 * b) % 230 for b in range(20)], [1 + b % 3 for b in range(20)], seed=dim).check()
+
+
+def block_rows(s, sms):
+    """Query rows of a unit, from the workspace that calls on `sms` multiprocessors ask for (tcgen05: one CTA each)."""
+    from paper_2607_04031_b200 import binding as tl
+    row = 2 * sms * (s.dim * 4 + 8)
+    need = tl.tree_attention_workspace_bytes(s.cache, s.batch, s.q.shape[1])
+    assert need % row == 0
+    return need // row
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("trees", ["tree", "random", "empty", "causal"])
+@pytest.mark.parametrize("sms", [2, 5])
+def test_blocks_of_256_rows(fmt, dim, trees, sms):
+    # 320 and 208 rows: a block and a quarter, and one not quite full
+    from paper_2607_04031_b200 import binding as tl
+    s = Step(fmt, 4, 8, dim, 16, [700, 333], [40, 26], trees=trees, seed=dim + sms)
+    with tl.option(tl.OPT_SM_LIMIT, sms):
+        s.check()
+        assert block_rows(s, sms) == 256
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_blocks_of_256_rows_and_what_is_masked(fmt):
+    # token 2's key and value hold what is not finite; rows that do not see it are as without it
+    from paper_2607_04031_b200 import binding as tl
+    clean, dirty = (Step(fmt, 4, 4, 128, 16, [400], [60], seed=22) for _ in range(2))
+    bad = torch.full((1, 4, 128), math.nan)
+    if fmt == "bf16":
+        pg, line = dirty.pool.place(0, torch.tensor([402]))
+        dirty.pool.v[pg, :, line] = math.inf
+        dirty.pool.k[pg, 1, line] = math.nan
+    else:
+        dirty.pool.write(0, torch.tensor([402]), bad, bad)
+    with tl.option(tl.OPT_SM_LIMIT, 1):
+        a, b = clean.run().float().cpu(), dirty.run().float().cpu()
+    hidden = ~clean.sees[0][:, 2]
+    assert bool(hidden.any()) and bool((~hidden).any())
+    # (bf16: weights may stay unrounded on the path that keeps such values out)
+    room = 2.0 ** -7 * a.abs() + 2.0 ** -8 * float(clean.pool.rows(0, 460)[1].abs().max()) if fmt == "bf16" else torch.zeros_like(a)
+    assert bool(((a - b).abs() <= room)[hidden].all())
+    assert bool((~torch.isfinite(b[~hidden])).all())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("counts,sms,rows", [([24, 24], 2, 256), ([23, 23], 2, 128), ([24, 24], 100, 128)])
+def test_the_choice_of_blocks_does_not_show(fmt, counts, sms, rows):
+    from paper_2607_04031_b200 import binding as tl
+    s = Step(fmt, 4, 8, 128, 16, [300, 290], counts, seed=5)
+    with tl.option(tl.OPT_SM_LIMIT, sms):
+        s.check()
+        if sms == 2:
+            assert block_rows(s, sms) == rows
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("tokens", [2, 3, 4, 5])
+def test_rows_around_the_choice_of_kernel(fmt, dim, tokens):
+    # 16 to 40 rows per key/value head, in a batch whose requests have fewer and more than the average
+    Step(fmt, 2, 8, dim, 32, [700, 65, 0], [tokens - 1, tokens, tokens + 1], seed=tokens).check()
