@@ -111,7 +111,7 @@ typedef enum {
                                 predecessor's completion from wrong expert offsets, so that its check after the wait
                                 must find them wrong and build them again; the output is the ordinary one.
                                 5 = in the next tl_tree_attention launch that runs on tcgen05 (more than 32 query rows per
-                                key/value head on average) CTA 0 never announces its first key tile, so that the waits for it
+                                key/value head on average, or more than 24 at head_dim 128) CTA 0 never announces its first key tile, so that the waits for it
                                 run out (detail 0xc00) and the CTA gives up; the rows it owns are undefined.
                                 The option resets itself to 0 when it is consumed. */
     TL_OPT_MOE_ROW_CAP,      /* grouped products: most token rows per tile; 0 (default): the library's choice (32, or 64 / 128 when
@@ -475,7 +475,8 @@ int tl_hw_box_load(const tl_hw_desc* desc, const void* d_src_tilemajor, uint64_t
  *
  * Formats.  TL_KV_BF16 holds the values rounded to bf16.  TL_KV_E4M3 and TL_KV_INT8 hold 8-bit codes and, per token
  * and head, one fp32 scale: with a = max |x| over the head_dim elements, scale = a * c with c = 1/448 (E4M3) or 1/127
- * (INT8) in fp32, code = x / scale (fp32) rounded to the nearest code, ties to even.  The value held is code * scale.  A row of zeros has scale 0; a row with an infinity or a NaN has scale NaN and reads back as NaN.
+ * (INT8) in fp32, code = x / scale (fp32) rounded to the nearest code, ties to even.  The value held is code * scale.
+ * A row of zeros has scale 0; a row with an infinity or a NaN has scale NaN and reads back as NaN.
  */
 typedef enum { TL_KV_BF16 = 0, TL_KV_E4M3 = 1, TL_KV_INT8 = 2 } tl_kv_format;
 typedef enum { TL_ELEM_BF16 = 0, TL_ELEM_F32 = 1 } tl_elem;
@@ -486,7 +487,8 @@ typedef struct tl_kv_cache {
     float* k_scale;             /* device, 16-byte aligned; NULL for TL_KV_BF16 */
     float* v_scale;
     int64_t pages;
-    int64_t page_stride, head_stride, token_stride;     /* elements, each a multiple of 16 bytes; all 0: packed */
+    int64_t page_stride, head_stride, token_stride;     /* elements, each a multiple of 16 bytes, a token's
+                                                           at most 2^26 bytes (else TL_ERR_UNSUPPORTED); all 0: packed */
     int64_t scale_page_stride, scale_head_stride;       /* floats, multiples of 4; both 0: packed [page][head][token].
                                                            The scales of a page's tokens are contiguous. */
     int32_t format;             /* tl_kv_format */
@@ -499,7 +501,7 @@ typedef struct tl_kv_cache {
  * i-th row stands at position start[b] + i of its sequence, which lives in page page_table[b][position / page_tokens]
  * of the pool.  All four arrays are read on the device, so a captured step follows their contents.  A position past
  * the table or a page number outside [0, pages) is never touched: the row is not written / not attended to / reads
- * back as zeros, and tl_device_status() reports it (TL_ERR_TIMEOUT, detail 0xA00).  Only the table's entries that
+ * back as zeros, and tl_device_status() reports it (TL_ERR_TIMEOUT, detail 0xa00).  Only the table's entries that
  * hold a request's tokens are read.  A sequence has at most 2^30 positions.
  */
 typedef struct tl_kv_batch {
@@ -554,7 +556,9 @@ int tl_tree_mask(const int32_t* d_parents, const int32_t* d_token_offsets, int r
  *   q_heads     a multiple of cache->heads.
  *   d_lse       NULL, or fp32 [tokens][q_heads]: natural logarithm of the sum of exp(scale * q . k).
  * Scores, softmax statistics and sums are fp32.  Scratch for sequences that several CTAs share comes from the
- * workspace (tl_tree_attention_workspace_bytes; tl_set_workspace or the internal one).  Asynchronous.
+ * workspace (tl_tree_attention_workspace_bytes; tl_set_workspace or the internal one).  A batch whose table and rows allow
+ * 2^31 tiles or more is refused (TL_ERR_UNSUPPORTED).  Waits inside the kernel are bounded (TL_OPT_WAIT_LIMIT_US; detail
+ * 0xc00 when one runs out).  Asynchronous.
  */
 int tl_tree_attention(const tl_kv_cache* cache, const tl_kv_batch* batch, const void* d_q, int64_t q_stride, int q_heads,
                       const uint32_t* d_mask, int mask_words, float scale, void* d_out, int64_t out_stride, float* d_lse,
@@ -581,7 +585,8 @@ size_t tl_tree_attention_workspace_bytes(const tl_kv_cache* cache, const tl_kv_b
  * vocabulary are fp64.
  *   d_accepted    int32 [requests][accepted_stride]: rows kept, within the request, root first, then -1.
  *   d_n_accepted  int32 [requests]: how many (0 for a request without rows).  d_next: int32 [requests] (-1 then).
- * vocab is at most 2^30.  A path ends at accepted_stride rows (>= 1): the last of them is treated as one without children.  Asynchronous.
+ * vocab is at most 2^30.  A path ends at accepted_stride rows (>= 1): the last of them is treated as one without
+ * children.  Asynchronous.
  */
 int tl_tree_verify(const float* d_target, int64_t target_stride, const float* d_draft, int64_t draft_stride, int64_t vocab,
                    const int32_t* d_tokens, const int32_t* d_parents, const int32_t* d_token_offsets, int requests,

@@ -17,6 +17,10 @@
 // as f16 can be where the contribution w_j v_j is large, and the softmax sum is that of w_j / vs_j.  The second product
 // takes w rounded to f16 (11 bits) with 8-bit caches, and as two bf16 terms (16 bits) with bf16 caches, whose eight bits
 // alone would put as much error into the result as its own rounding does; the sum takes w in fp32.
+//
+// What bounds it: the floor is one reading of the cache.  32 requests of one token (8 rows a head) over 4100 positions, E4M3:
+// 60.6 us, 3.5 TB/s, 0.53 of a plain copy; every byte is read once, the issue slots are 36 % in use and DRAM 43 %: the chain
+// from scores over maximum and exponential to the second product, with the 12 warps per SM that its registers allow.
 #pragma once
 
 #include "tl_attend.cuh"

@@ -2,13 +2,14 @@
 // tensor cores.
 //
 // One CTA per SM, five warpgroups: two for softmax (streams A and B), two of producers, and one whose first warp issues
-// the matrix instructions; registers are moved from the last three to the first two.  A stream is an accumulator O (128 rows x dim) and a score tile S (128 x 128) in tensor memory.
+// the matrix instructions; registers are moved from the last three to the first two.  A stream is an accumulator O
+// (128 rows x dim) and a score tile S (128 x 128) in tensor memory.
 //   kBlocks = 2  the streams hold different rows (256 rows a unit) and use every key/value tile together: each fetched
 //                and converted element serves 256 rows;
 //   kBlocks = 1  the streams hold the same 128 rows and take the tiles in turn; their sums are joined at the end.
 // Either way one stream's products run while the other's softmax does.  Per tile and stream: S = Q K^T (both operands in
-// shared memory, 128-byte swizzle), the warpgroup reads S, writes the weights back over it as 16-bit values, and O += P V takes P from tensor memory and V from shared memory as an MN-major
-// operand, so neither P nor V^T is ever laid out again.
+// shared memory, 128-byte swizzle), the warpgroup reads S, writes the weights back over it as 16-bit values, and O += P V
+// takes P from tensor memory and V from shared memory as an MN-major operand, so neither P nor V^T is ever laid out again.
 //
 // The row maximum is allowed to lag: weights are taken against the maximum known so far, and only when a score exceeds
 // it by more than 2^8 are O, the sum and the tile's earlier weights rescaled; sums are fp32 and f16 has room for 2^15, so
@@ -18,6 +19,12 @@
 // 8-bit tiles are fetched by the producers one tile ahead, converted and stored swizzled; full bf16 tiles
 // come by TMA (128-byte-swizzled boxes, one per page and 64 dimensions); a tile with positions past the end, or with a
 // page outside the pool, goes through registers too, with zeros in those places.
+//
+// What bounds it: the floor is the larger of one reading of the cache and the two products.  8 trees of 32 over 8000 (256 rows
+// a head, E4M3): 111 us, 400 TFLOP/s; 1 tree of 64 over 100000 (512 rows, bf16): 312 to 319 us, 660 TFLOP/s; 48 trees of 16 over
+// 6000 (128 rows, INT8): 242 us, 2.0 TB/s.  A step of two streams takes some 5200 clocks: 3700 for the softmax of a stream,
+// bound by the latency of reading scores, exponentials and writing weights (the exponentials alone are 2048), 1500
+// from its last weight over the second product to the next scores; the tensor pipe is in use for 29 to 38 % of the time.
 #pragma once
 
 #include "tl_attend.cuh"
@@ -148,13 +155,13 @@ __device__ __forceinline__ F2 f2_add(F2 a, F2 b) {
 // Barriers of the CTA.  Every wait on them is bounded.
 struct TcBars {
     uint64_t q_full;                     // 8 softmax warps: queries are in place, the last unit's accumulators are read
-    uint64_t k_full[3], k_empty[3], v_full[3], v_empty[3];
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
     uint64_t s_full[2], p_full[2], pv_done[2];
     uint64_t exchange;                   // 8 softmax warps: statistics of the two streams are in place
     uint64_t drained;                    // the issuing thread's last commit, when it gives up
     uint32_t abort_flag, tmem_base;
-    uint32_t meta[3];                    // per value stage: groups of 16 positions that should have a page and have none
-    alignas(8) uint8_t odd[3][kTcProducers];        // per value stage and producer warp: values that are not finite were taken out
+    uint32_t meta[2];                    // per value stage: groups of 16 positions that should have a page and have none
+    alignas(8) uint8_t odd[2][kTcProducers];        // per value stage and producer warp: values that are not finite were taken out
 };
 static_assert(sizeof(TcBars) <= 256, "barrier block");
 
@@ -173,7 +180,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
 
     if (threadIdx.x == 0) {
         mbar_init(&bars.q_full, kTcSoftmaxWarps);
-        for (int i = 0; i < 3; ++i) {
+        for (int i = 0; i < 2; ++i) {
             mbar_init(&bars.k_full[i], kTcProducers);
             mbar_init(&bars.k_empty[i], 1);
             mbar_init(&bars.v_full[i], kTcProducers);
