@@ -438,3 +438,38 @@ def test_the_choice_of_blocks_does_not_show(fmt, counts, sms, rows):
 def test_rows_around_the_choice_of_kernel(fmt, dim, tokens):
     # 16 to 40 rows per key/value head, in a batch whose requests have fewer and more than the average
     Step(fmt, 2, 8, dim, 32, [700, 65, 0], [tokens - 1, tokens, tokens + 1], seed=tokens).check()
+
+
+def test_a_batch_of_too_many_tiles_is_refused():
+    # 2^16 requests whose tables have room for 2^26 positions each: no memory is looked at
+    from paper_2607_04031_b200 import binding as tl
+    s = Step("int8", 2, 4, 128, 1024, [100], [1], seed=1)
+    s.check()
+    b = tl.KvBatch()
+    b.page_table, b.start, b.token_offsets = s.batch.page_table, s.batch.start, s.batch.token_offsets
+    b.table_stride, b.requests, b.tokens = 2 ** 16, 2 ** 16, 2 ** 16
+    b._ref = tl.ctypes.byref(b)
+    assert tl.tree_attention_workspace_bytes(s.cache, b, 8) == 0
+    q = torch.empty(2 ** 16, 8, 128, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(tl.TileLensError) as e:
+        tl.tree_attention(s.cache, b, q, torch.empty_like(q))
+    assert e.value.status == 2
+
+
+@pytest.mark.parametrize("counts", [[3], [50]])
+def test_the_workspace_may_be_the_callers(counts):
+    from paper_2607_04031_b200 import binding as tl
+    s = Step("e4m3", 2, 4, 128, 32, [3000], counts, seed=12)
+    a = s.run().clone()
+    need = tl.tree_attention_workspace_bytes(s.cache, s.batch, s.q.shape[1])
+    ws = torch.full((need + 256,), 7, dtype=torch.uint8, device="cuda")
+    try:
+        tl.set_workspace(ws[:need])
+        assert torch.equal(a, s.run())
+        assert bool((ws[need:] == 7).all()) and not bool((ws[:need] == 7).all())
+        tl.set_workspace(ws[:need - 256])
+        with pytest.raises(tl.TileLensError) as e:
+            s.run()
+        assert e.value.status == 6
+    finally:
+        tl.set_workspace(None)

@@ -116,3 +116,10 @@ def test_binding_refuses_wrong_tensors(tl):
     import torch
     with pytest.raises(ValueError, match="CUDA|expected"):
         tl.kv_cache(torch.zeros(1, 1, 16, 64, dtype=torch.int8), torch.zeros(1, 1, 16, 64, dtype=torch.int8))
+
+
+def test_tokens_further_apart_than_32_bit_offsets_allow_are_refused(tl):
+    # INT8: 2^26 bytes between tokens are the most; bf16: 2^25 elements
+    for fmt, most in ((tl.KV_INT8, 2 ** 26), (tl.KV_BF16, 2 ** 25)):
+        wide = dict(format=fmt, page_stride=64 * most, head_stride=128, token_stride=most + 16)
+        assert _append(tl, _cache(tl, **wide)) == 2 and _attend(tl, _cache(tl, **wide)) == 2
