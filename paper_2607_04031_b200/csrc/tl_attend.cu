@@ -10,12 +10,65 @@ namespace tl {
 // borders inside one unit share its rows out among themselves, and so do the blocks of a border (one per 16 rows of the
 // unit: with one block a border, 256-row units took 33 to 60 us here, a chain of dependent loads per row).
 constexpr int kCombineThreads = 256, kCombineRows = 16;
+// From this many parts of a unit on four lanes share an element's: units in so many parts are few or narrow, and most
+// threads would have nothing to do.  Whole calls over 4100 positions, one lane / four lanes: 1 request of 16 rows E4M3 (33
+// parts) 35.8 / 27.6 us, bf16 of 32 rows (17) 31.7 / 29.7, 4 requests of 16 rows E4M3 (14) 35.8 / 33.8; 512 rows over 16000
+// (10 parts of 256 rows) 76.8 / 78.8.
+constexpr int kCombineMany = 12;
+
+struct CombineUnit {
+    AttendPlace w;
+    int c0, c1;                          // the CTAs that hold parts
+    int rows, share, shares;
+};
+template <int kLanes>
+__device__ __forceinline__ void combine_unit(const AttendParams& p, const CombineUnit& u, int dim) {
+    const int vecs = dim / 4;
+    // (a row has 16 elements of four dimensions at least: with four lanes each, a warp is inside or outside as a whole)
+    for (int x = u.share * kCombineThreads + int(threadIdx.x); x < u.rows * vecs * kLanes; x += u.shares * kCombineThreads) {
+        const int e = x / kLanes, sub = x % kLanes;
+        const int r = e / vecs, d = e % vecs * 4;
+        // CTA c0 ends inside the unit it began (its second slot); the others begin inside it (their first)
+        auto slot = [&](int c) { return int64_t(c) * 2 + (c == u.c0 ? 1 : 0); };
+        float top = -INFINITY;
+#pragma unroll 4
+        for (int c = u.c0 + sub; c <= u.c1; c += kLanes) top = fmaxf(top, p.part_ml[slot(c) * p.rows_block + r].x);
+#pragma unroll
+        for (int k = 1; k < kLanes; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+        const float use = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int c = u.c0 + sub; c <= u.c1; c += kLanes) {
+            const float2 ml = p.part_ml[slot(c) * p.rows_block + r];
+            const float4 v = *reinterpret_cast<const float4*>(p.part + (slot(c) * p.rows_block + r) * dim + d);
+            const float f = ex2(ml.x - use);
+            sum = fmaf(ml.y, f, sum);
+            o.x = fmaf(v.x, f, o.x), o.y = fmaf(v.y, f, o.y), o.z = fmaf(v.z, f, o.z), o.w = fmaf(v.w, f, o.w);
+        }
+#pragma unroll
+        for (int k = 1; k < kLanes; k <<= 1) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, k);
+            o.x += __shfl_xor_sync(0xffffffffu, o.x, k), o.y += __shfl_xor_sync(0xffffffffu, o.y, k);
+            o.z += __shfl_xor_sync(0xffffffffu, o.z, k), o.w += __shfl_xor_sync(0xffffffffu, o.w, k);
+        }
+        if (kLanes > 1 && sub != 0) continue;
+        const AttendPlace& w = u.w;
+        const int row = w.block * p.rows_block + r, tok = row / p.group, hq = w.head * p.group + row % p.group;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        *reinterpret_cast<uint2*>(p.out + int64_t(w.a.r.first + tok) * p.out_stride + int64_t(hq) * dim + d) =
+            make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        if (p.lse && d == 0) p.lse[int64_t(w.a.r.first + tok) * p.q_heads + hq] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+    }
+}
+
 __global__ void __launch_bounds__(kCombineThreads) attend_combine_kernel(const AttendParams p, int dim) {
     pdl_launch_dependents();
     // (The lengths may be read ahead of the wait: every CTA of the attention kernel has let this one start after its own
     // wait, so whatever wrote them is over.)
     int per, border, border_end;
-    AttendPlace w;
+    CombineUnit u;
+    AttendPlace& w = u.w;
     if (!attend_range(p, int(blockIdx.x) + 1, &per, &border, &border_end, &w) || w.tile == 0) {
         // Nothing to join: the line ends ahead of the border, or the border lies between two units.  One block waits all the
         // same: what follows waits for this grid alone, which must not be over before the attention kernel is.
@@ -23,35 +76,12 @@ __global__ void __launch_bounds__(kCombineThreads) attend_combine_kernel(const A
         return;
     }
     const int u0 = border - w.tile, u1 = u0 + w.a.tiles;
-    const int c0 = int(uint32_t(u0) / uint32_t(per)), c1 = int(uint32_t(u1 - 1) / uint32_t(per));
-    const int share = (int(blockIdx.x) - c0) * int(gridDim.y) + int(blockIdx.y), shares = (c1 - c0) * int(gridDim.y);
-    const int rows = min(p.rows_block, w.a.r.n * p.group - w.block * p.rows_block);
-    const int vecs = dim / 4;
+    u.c0 = int(uint32_t(u0) / uint32_t(per)), u.c1 = int(uint32_t(u1 - 1) / uint32_t(per));
+    u.share = (int(blockIdx.x) - u.c0) * int(gridDim.y) + int(blockIdx.y), u.shares = (u.c1 - u.c0) * int(gridDim.y);
+    u.rows = min(p.rows_block, w.a.r.n * p.group - w.block * p.rows_block);
     pdl_wait();
-    for (int e = share * kCombineThreads + threadIdx.x; e < rows * vecs; e += shares * kCombineThreads) {
-        const int r = e / vecs, d = e % vecs * 4;
-        // CTA c0 ends inside the unit it began (its second slot); the others begin inside it (their first)
-        auto slot = [&](int c) { return int64_t(c) * 2 + (c == c0 ? 1 : 0); };
-        float top = -INFINITY;
-#pragma unroll 4
-        for (int c = c0; c <= c1; ++c) top = fmaxf(top, p.part_ml[slot(c) * p.rows_block + r].x);
-        const float use = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int c = c0; c <= c1; ++c) {
-            const float2 ml = p.part_ml[slot(c) * p.rows_block + r];
-            const float4 v = *reinterpret_cast<const float4*>(p.part + (slot(c) * p.rows_block + r) * dim + d);
-            const float f = ex2(ml.x - use);
-            sum = fmaf(ml.y, f, sum);
-            o.x = fmaf(v.x, f, o.x), o.y = fmaf(v.y, f, o.y), o.z = fmaf(v.z, f, o.z), o.w = fmaf(v.w, f, o.w);
-        }
-        const int row = w.block * p.rows_block + r, tok = row / p.group, hq = w.head * p.group + row % p.group;
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        *reinterpret_cast<uint2*>(p.out + int64_t(w.a.r.first + tok) * p.out_stride + int64_t(hq) * dim + d) =
-            make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-        if (p.lse && d == 0) p.lse[int64_t(w.a.r.first + tok) * p.q_heads + hq] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
-    }
+    if (u.c1 - u.c0 + 1 >= kCombineMany) combine_unit<4>(p, u, dim);
+    else combine_unit<1>(p, u, dim);
 }
 
 int attend_small_bf16(bool, int, int, int*, int*, const AttendParams*, int, cudaStream_t);
