@@ -21,8 +21,8 @@
 // page outside the pool, goes through registers too, with zeros in those places.
 //
 // What bounds it: the floor is the larger of one reading of the cache and the two products.  8 trees of 32 over 8000 (256 rows
-// a head, E4M3): 111 us, 400 TFLOP/s; 1 tree of 64 over 100000 (512 rows, bf16): 312 to 319 us, 660 TFLOP/s; 48 trees of 16 over
-// 6000 (128 rows, INT8): 242 us, 2.0 TB/s.  A step of two streams takes some 5200 clocks: 3700 for the softmax of a stream,
+// a head, E4M3): 111 us, 400 TFLOP/s; 1 tree of 64 over 100000 (512 rows, bf16): 312 to 324 us, 650 to 670 TFLOP/s; 48 trees of 16 over
+// 6000 (128 rows, INT8): 241 to 247 us, 2.0 TB/s.  A step of two streams takes some 5200 clocks: 3700 for the softmax of a stream,
 // bound by the latency of reading scores, exponentials and writing weights (the exponentials alone are 2048), 1500
 // from its last weight over the second product to the next scores; the tensor pipe is in use for 29 to 38 % of the time.
 #pragma once
