@@ -624,8 +624,8 @@ def tree_verify(target: torch.Tensor, draft: torch.Tensor | None, tokens: torch.
                 n_accepted: torch.Tensor, next_token: torch.Tensor, stream=None):
     """Which drafts the target's distribution keeps, and the token that follows them.
 
-    target, draft: fp32 [tokens, vocab] (draft None: the drafts were chosen without chance); tokens, parents: int32
-    [tokens]; accept: fp32 [tokens] and sample: fp32 [requests], uniform in [0, 1).  Written: accepted int32 [requests, n]
+    target, draft: fp32 [tokens, vocab], every row in memory of its own (draft None: the drafts were chosen without chance);
+    tokens, parents: int32 [tokens]; accept: fp32 [tokens] and sample: fp32 [requests], uniform in [0, 1).  Written: accepted int32 [requests, n]
     (rows kept within the request, root first, then -1), n_accepted and next_token int32 [requests].
     """
     shape, ts, f32 = target.shape, target.stride(), torch.float32
@@ -638,11 +638,11 @@ def tree_verify(target: torch.Tensor, draft: torch.Tensor | None, tokens: torch.
         ds = draft.stride()
         if draft.dtype is not f32 or not draft.is_cuda or draft.shape != shape or (ds[1] != 1 and vocab > 1):
             raise ValueError("draft: expected target's shape, type and contiguous rows")
-        dp, ds = draft.data_ptr(), max(ds[0], vocab)
+        dp, ds = draft.data_ptr(), ds[0] if rows > 1 else vocab
     for t, name, n in ((accept, "accept", rows), (sample, "sample", requests)):
         if t.dtype is not f32 or not t.is_cuda or t.shape != (n,) or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous CUDA tensor of {n} fp32 numbers")
-    st = lib().tl_tree_verify(target.data_ptr(), max(ts[0], vocab), dp, ds, vocab, _int32(tokens, "tokens", (rows,)),
+    st = lib().tl_tree_verify(target.data_ptr(), ts[0] if rows > 1 else vocab, dp, ds, vocab, _int32(tokens, "tokens", (rows,)),
                               _int32(parents, "parents", (rows,)), _int32(token_offsets, "token_offsets", (requests + 1,)),
                               requests, rows, accept.data_ptr(), sample.data_ptr(),
                               _int32(accepted, "accepted", (requests, most)), most, _int32(n_accepted, "n_accepted", (requests,)),
