@@ -174,7 +174,7 @@ int tl_tree_attention(const tl_kv_cache* cache, const tl_kv_batch* batch, const 
     const int64_t wide = int64_t(q_heads) * cache->head_dim;
     if (!d_q || !d_out || q_stride < wide || out_stride < wide) return TL_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(d_q) % 16 || reinterpret_cast<uintptr_t>(d_out) % 16 || q_stride % 8 || out_stride % 8 ||
-        reinterpret_cast<uintptr_t>(d_mask) % 4 || reinterpret_cast<uintptr_t>(d_lse) % 4)
+        !words_aligned(d_mask, d_lse))
         return TL_ERR_ALIGNMENT;
     if (opt(TL_OPT_PLAN_AS_IF_SMS)) return TL_ERR_INVALID_ARG;
     ApiLock lock;

@@ -37,6 +37,10 @@ constexpr int64_t kKvMaxTokens = int64_t(1) << 30;         // of one sequence
 int kv_view(const tl_kv_cache* c, KvView* out);
 int kv_batch_view(const tl_kv_batch* b, KvBatchView* out);
 
+// Whether each of the arrays (NULL ones aside) starts on a boundary of its 4-byte elements.
+template <typename... P>
+inline bool words_aligned(const P*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 3u) == 0; }
+
 inline int kv_item(int format) { return format == TL_KV_BF16 ? 2 : 1; }
 
 #ifdef __CUDACC__

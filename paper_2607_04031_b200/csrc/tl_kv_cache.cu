@@ -58,9 +58,7 @@ int kv_batch_view(const tl_kv_batch* b, KvBatchView* out) {
     if (!b || !out || b->requests < 0 || b->tokens < 0) return TL_ERR_INVALID_ARG;
     if (b->requests > 0 && (!b->page_table || !b->start || !b->token_offsets || b->table_stride < 1)) return TL_ERR_INVALID_ARG;
     if (b->table_stride > (int64_t(1) << 40)) return TL_ERR_INVALID_ARG;
-    if (reinterpret_cast<uintptr_t>(b->page_table) % 4 || reinterpret_cast<uintptr_t>(b->start) % 4 ||
-        reinterpret_cast<uintptr_t>(b->token_offsets) % 4)
-        return TL_ERR_ALIGNMENT;
+    if (!words_aligned(b->page_table, b->start, b->token_offsets)) return TL_ERR_ALIGNMENT;
     out->page_table = b->page_table;
     out->start = b->start;
     out->offsets = b->token_offsets;
@@ -500,6 +498,7 @@ int tl_kv_commit(const tl_kv_cache* cache, const tl_kv_batch* batch, const int32
     if (int rc = kv_batch_view(batch, &p.batch)) return rc;
     if (p.batch.requests == 0) return TL_OK;
     if (!d_accepted || !d_n_accepted || accepted_stride < 1) return TL_ERR_INVALID_ARG;
+    if (!words_aligned(d_accepted, d_n_accepted, d_new_start)) return TL_ERR_ALIGNMENT;
     if (opt(TL_OPT_PLAN_AS_IF_SMS)) return TL_ERR_INVALID_ARG;
     ApiLock lock;
     if (int rc = ensure_control()) return rc;
@@ -520,6 +519,7 @@ int tl_tree_mask(const int32_t* d_parents, const int32_t* d_token_offsets, int r
     if (requests < 0 || tokens < 0 || mask_words < 1) return TL_ERR_INVALID_ARG;
     if (requests == 0 || tokens == 0) return TL_OK;
     if (!d_parents || !d_token_offsets || !d_mask) return TL_ERR_INVALID_ARG;
+    if (!words_aligned(d_parents, d_token_offsets, d_mask)) return TL_ERR_ALIGNMENT;
     if (opt(TL_OPT_PLAN_AS_IF_SMS)) return TL_ERR_INVALID_ARG;
     ApiLock lock;
     return kv_launch(tree_mask_kernel, dim3(unsigned(ceil_div(tokens, 8))), 256, static_cast<cudaStream_t>(cuda_stream),

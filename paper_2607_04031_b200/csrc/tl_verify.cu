@@ -380,6 +380,8 @@ int tl_tree_verify(const float* d_target, int64_t target_stride, const float* d_
     if (!d_token_offsets || !d_accepted || !d_n_accepted || !d_next || !d_sample) return TL_ERR_INVALID_ARG;
     if (tokens > 0 && (!d_target || !d_tokens || !d_parents || !d_accept)) return TL_ERR_INVALID_ARG;
     if (target_stride < vocab || (d_draft && draft_stride < vocab)) return TL_ERR_INVALID_ARG;
+    if (!words_aligned(d_target, d_draft, d_tokens, d_parents, d_token_offsets, d_accept, d_sample, d_accepted, d_n_accepted, d_next))
+        return TL_ERR_ALIGNMENT;
     if (opt(TL_OPT_PLAN_AS_IF_SMS)) return TL_ERR_INVALID_ARG;
     ApiLock lock;
     if (int rc = ensure_device_info()) return rc;

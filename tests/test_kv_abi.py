@@ -123,3 +123,17 @@ def test_tokens_further_apart_than_32_bit_offsets_allow_are_refused(tl):
     for fmt, most in ((tl.KV_INT8, 2 ** 26), (tl.KV_BF16, 2 ** 25)):
         wide = dict(format=fmt, page_stride=64 * most, head_stride=128, token_stride=most + 16)
         assert _append(tl, _cache(tl, **wide)) == 2 and _attend(tl, _cache(tl, **wide)) == 2
+
+
+def test_pointers_off_their_elements_are_refused(tl):
+    # every array these calls read or write in words of four bytes: two bytes off it would be a misaligned access
+    names = ("target", "draft", "tokens", "parents", "offs", "accept", "sample", "acc", "n", "nxt")
+    for name in names:
+        a = {**{k: P for k in names}, name: P + 2}
+        assert tl.lib().tl_tree_verify(a["target"], 100, a["draft"], 100, 100, a["tokens"], a["parents"], a["offs"], 2, 6, a["accept"],
+                                       a["sample"], a["acc"], 4, a["n"], a["nxt"], None) == 3, name
+    for i in range(3):
+        a = [P + 2 * (k == i) for k in range(3)]
+        assert tl.lib().tl_tree_mask(a[0], a[1], 1, 4, a[2], 1, None) == 3
+        c, b = _cache(tl), _batch(tl)
+        assert tl.lib().tl_kv_commit(ctypes.byref(c), ctypes.byref(b), a[0], 4, a[1], a[2], None) == 3
