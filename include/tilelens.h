@@ -475,7 +475,8 @@ int tl_hw_box_load(const tl_hw_desc* desc, const void* d_src_tilemajor, uint64_t
  *
  * Formats.  TL_KV_BF16 holds the values rounded to bf16.  TL_KV_E4M3 and TL_KV_INT8 hold 8-bit codes and, per token
  * and head, one fp32 scale: with a = max |x| over the head_dim elements, scale = a * c with c = 1/448 (E4M3) or 1/127
- * (INT8) in fp32, code = x / scale (fp32) rounded to the nearest code, ties to even.  The value held is code * scale.
+ * (INT8) in fp32, code = x / scale (fp32) rounded to the nearest code, ties to even (the largest code at most: where the
+ * scale is a subnormal number, x / scale may be larger).  The value held is code * scale.
  * A row of zeros has scale 0; a row with an infinity or a NaN has scale NaN and reads back as NaN.
  */
 typedef enum { TL_KV_BF16 = 0, TL_KV_E4M3 = 1, TL_KV_INT8 = 2 } tl_kv_format;

@@ -245,8 +245,9 @@ __global__ void __launch_bounds__(kCopyThreads) kv_append_kernel(const KvCopyPar
             const uint32_t group = (kLanes == 32 ? 0xffffffffu : ((1u << kLanes) - 1u) << (sub * kLanes));
 #pragma unroll
             for (int d = kLanes / 2; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(group, top, d));
+            constexpr float kTop = kFmt == TL_KV_E4M3 ? 448.0f : 127.0f;
             const bool finite = top < 0x7f800000u;
-            const float s = finite ? __fmul_rn(__uint_as_float(top), kFmt == TL_KV_E4M3 ? 1.0f / 448.0f : 1.0f / 127.0f) : __uint_as_float(0x7fc00000u);
+            const float s = finite ? __fmul_rn(__uint_as_float(top), 1.0f / kTop) : __uint_as_float(0x7fc00000u);
             uint32_t lo = 0, hi = 0;
             if (finite && s > 0.0f) {
                 float y[8];
@@ -261,8 +262,9 @@ __global__ void __launch_bounds__(kCopyThreads) kv_append_kernel(const KvCopyPar
                         y[e] = __fmaf_rn(__fmaf_rn(-q, s, x[e]), inv, q);
                     }
                 } else {
+                    // (a subnormal scale is rounded to a few bits, down to two thirds of top * c: the quotient is clamped)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = __fdiv_rn(x[e], s);
+                    for (int e = 0; e < 8; ++e) y[e] = fminf(fmaxf(__fdiv_rn(x[e], s), -kTop), kTop);
                 }
                 if (kFmt == TL_KV_E4M3) {
                     // (the saturating conversion keeps the last bit of a quotient just above 448)
@@ -274,7 +276,8 @@ __global__ void __launch_bounds__(kCopyThreads) kv_append_kernel(const KvCopyPar
                     lo = two(y[0], y[1]) | two(y[2], y[3]) << 16;
                     hi = two(y[4], y[5]) | two(y[6], y[7]) << 16;
                 } else {
-                    // |y| <= 127 (1 + 2^-22), so rounding needs no clamp; 1.5 x 2^23 leaves the integer in the low bits
+                    // |y| <= 127 (1 + 2^-22) where the scale is normal, so rounding needs no clamp; 1.5 x 2^23 leaves the integer in
+                    // the low bits
                     uint32_t z[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) z[e] = __float_as_uint(__fadd_rn(y[e], 12582912.0f));
