@@ -364,9 +364,10 @@ attend_kernel(const AttendParams p) {
                     for (int h = 0; h < 2; ++h) {
                         float x = fmaxf(top[mt][h], __shfl_xor_sync(0xffffffffu, top[mt][h], 1));
                         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-                        const float m_new = fmaxf(m[mt][h], x);
-                        const float f = m_new == -INFINITY ? 1.0f : ex2(m[mt][h] - m_new);
-                        m[mt][h] = m_new;
+                        // (by the row's own scores: what other rows see leaves its bits alone)
+                        const bool up = x > m[mt][h] + 8.0f;
+                        const float f = up ? ex2(m[mt][h] - x) : 1.0f;
+                        m[mt][h] = up ? x : m[mt][h];
                         l[mt][h] *= f;
 #pragma unroll
                         for (int j = 0; j < S::kNTiles; ++j) {

@@ -13,7 +13,7 @@
 //
 // The row maximum is allowed to lag: weights are taken against the maximum known so far, and only when a score exceeds
 // it by more than 2^8 are O, the sum and the tile's earlier weights rescaled; sums are fp32 and f16 has room for 2^15, so
-// the lag costs no accuracy.  Scales of 8-bit caches enter as in the kernel for few rows (key's
+// the lag costs no accuracy.  Rows are rescaled by their own scores alone: a row's bits do not depend on what its neighbours see.  Scales of 8-bit caches enter as in the kernel for few rows (key's
 // scale on the score, value's in the exponent), q is f16 scaled by a power of two per row; conversion to f16 is exact.
 //
 // 8-bit tiles are fetched by the producers one tile ahead, converted and stored swizzled; full bf16 tiles
@@ -402,9 +402,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             for (int h = 0; h < 4; ++h) {
                                 top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
                                 top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
-                                const float m_new = fmaxf(m[h], top[h]);
-                                f[h] = ex2(m[h] - m_new);
-                                m[h] = m_new;
+                                const bool up = top[h] > m[h] + 8.0f;        // (by the row's own scores)
+                                f[h] = up ? ex2(m[h] - top[h]) : 1.0f;
+                                m[h] = up ? top[h] : m[h];
                                 l[h] *= f[h];
                                 sum[h] = f2_mul(sum[h], F2{f[h], f[h]});
                             }
