@@ -74,6 +74,7 @@ attend_kernel(const AttendParams p) {
     float* const row_fac = stat_l + S::kWarps * S::kRows;                             // [row]
     float* const row_m = row_fac + S::kRows;                                          // [row] joined maximum and sum
     float* const row_l = row_m + S::kRows;
+    float* const nan_taken = row_l + S::kRows;                                        // E4M3: not 0 when NaN codes were taken out
     const int lane = int(lane_id()), warp = int(threadIdx.x) / 32, g = lane >> 2, t = lane & 3;
     const uint32_t ring = smem_u32(smem) + uint32_t(warp * S::kStages * S::kStageBytes);
     const char* const ring_gen = smem + warp * S::kStages * S::kStageBytes;
@@ -159,6 +160,7 @@ attend_kernel(const AttendParams p) {
 #pragma unroll
         for (int i = 0; i < S::kStages - S::kSub; ++i) issue(i);
 
+        if (kFmt == TL_KV_E4M3 && threadIdx.x == 0) *nan_taken = 0.0f;
         // the query rows as A fragments: warp by warp, one row at a time
         for (int r = warp; r < S::kRows; r += S::kWarps) {
             const int row = w.block * S::kRows + r;
@@ -408,7 +410,7 @@ attend_kernel(const AttendParams p) {
                 const char* const vst = st[u] + 16 * S::kRowBytes;
                 if (kBf16 && edge[u]) {
                     // A value may be infinite or NaN for a token that other rows see: its product with a masked weight of 0
-                    // must not reach this row.  (8-bit codes are always finite, and positions past the end were filled with 0.)
+                    // must not reach this row.  (Positions past the end were filled with 0; INT8 codes are always finite.)
                     bool odd = false;
 #pragma unroll
                     for (int k = 0; k < 4 * S::kVChunks; ++k) {
@@ -455,6 +457,20 @@ attend_kernel(const AttendParams p) {
                             const uint2 x = *reinterpret_cast<const uint2*>(src);
                             v[k][0] = x.x, v[k][1 % kWords] = x.y;
                         }
+                    }
+                    if (kFmt == TL_KV_E4M3 && edge[u]) {
+                        // Among the step's own tokens, of which rows see different ones: a NaN code stays out of the product (a weight
+                        // of 0 would not keep it out), and the rows that see it get theirs when the warps are joined.
+                        uint32_t any = 0;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+#pragma unroll
+                            for (int q = 0; q < kWords; ++q) {
+                                const uint32_t bad = e4m3_nan_bytes(v[k][q]);
+                                v[k][q] &= ~bad;
+                                any |= bad;
+                            }
+                        if (any != 0) *nan_taken = 1.0f;
                     }
 #pragma unroll
                     for (int q = 0; q < kWords; ++q) {
@@ -541,6 +557,21 @@ attend_kernel(const AttendParams p) {
             for (int k = 0; k < S::kWarps; ++k) {
                 const float4 v = *reinterpret_cast<const float4*>(join + (k * S::kRows + r) * kDim + d);
                 sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+            }
+            if (kFmt == TL_KV_E4M3 && *nan_taken != 0.0f) {
+                const int tok = (w.block * S::kRows + r) / p.group;
+                for (int pos = t0 * S::kTile; pos < min(len, t1 * S::kTile); ++pos) {
+                    if (!attend_sees(p, w.a.r.first + tok, tok, pos - start)) continue;
+                    const int page = table[pos >> p.cache.page_shift];
+                    if (page < 0 || page >= p.cache.pages) continue;
+                    const uint32_t bad = e4m3_nan_bytes(*reinterpret_cast<const uint32_t*>(
+                        v_head + int64_t(page) * p.cache.page_stride + int64_t(pos & pos_mask) * p.cache.token_stride + d));
+                    const float nan = __uint_as_float(0x7fc00000u);
+                    if (bad & 0xffu) sum.x = nan;
+                    if (bad & 0xff00u) sum.y = nan;
+                    if (bad & 0xff0000u) sum.z = nan;
+                    if (bad & 0xff000000u) sum.w = nan;
+                }
             }
             if (whole) {
                 const int row = w.block * S::kRows + r, tok = row / p.group, hq = w.head * p.group + row % p.group;

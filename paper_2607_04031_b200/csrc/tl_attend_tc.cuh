@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     ++s_count;
                     tc_fence_after_sync();
                     const uint32_t meta = bars.meta[at];
-                    if (kBf16) odd |= *reinterpret_cast<const uint64_t*>(bars.odd[at]) != 0;
+                    if (kFmt != TL_KV_INT8) odd |= *reinterpret_cast<const uint64_t*>(bars.odd[at]) != 0;
                     const int pos0 = (t0 + n) * kTcTile;
                     const bool edge = pos0 + kTcTile > w.a.r.start || meta != 0;
                     const float* const ks = scales + at * 3 * kTcTile + 2 * t4;
@@ -546,6 +546,23 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                                 }
                             }
                         }
+                        if (kFmt == TL_KV_E4M3 && odd_all) {
+                            // NaN codes alike: which of this row's 32 dimensions see one
+                            uint32_t nan = 0;
+                            const int from = max(w.a.r.start, t0 * kTcTile), to = min(w.a.r.len, t1 * kTcTile);
+#pragma unroll 1
+                            for (int pos = from; pos < to; ++pos) {
+                                if (!attend_sees(p, w.a.r.first + tok, tok, pos - w.a.r.start)) continue;
+                                const int page = p.batch.page_table[int64_t(w.b) * p.batch.table_stride + (pos >> p.cache.page_shift)];
+                                if (page < 0 || page >= p.cache.pages) continue;
+                                const char* const codes = p.cache.base[1] + int64_t(page) * p.cache.page_stride + int64_t(w.head) * p.cache.head_stride +
+                                                          int64_t(pos & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride + c * 32;
+#pragma unroll 1
+                                for (int i = 0; i < 32; ++i) nan |= ((codes[i] & 0x7f) == 0x7f ? 1u : 0u) << i;
+                            }
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = nan >> i & 1u ? __uint_as_float(0x7fc00000u) : o[i];
+                        }
                         if (whole) {
                             uint4* dst = reinterpret_cast<uint4*>(p.out + int64_t(w.a.r.first + tok) * p.out_stride + int64_t(hq) * kDim + c * 32);
 #pragma unroll
@@ -657,6 +674,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                                    (in ? pos & pos_mask : 0));
                         sc_lack = !in;                                       // (zeroed at its use: here it would be waited for)
                     };
+                    // Values of a tile whose rows from own_from on are the step's own tokens.  Query rows differ in what they see of those,
+                    // so an E4M3 NaN stays out of the product (a weight of 0 would not keep it out).  True: there was one.
+                    auto take_nan_out = [&](int own_from) -> bool {
+                        auto clean = [](uint4& v) -> bool {
+                            const uint4 bad = make_uint4(e4m3_nan_bytes(v.x), e4m3_nan_bytes(v.y), e4m3_nan_bytes(v.z), e4m3_nan_bytes(v.w));
+                            v = make_uint4(v.x & ~bad.x, v.y & ~bad.y, v.z & ~bad.z, v.w & ~bad.w);
+                            return (bad.x | bad.y | bad.z | bad.w) != 0;
+                        };
+                        bool odd = row0 + (kRounds - 1) * kRowsPer >= own_from && !lack && clean(last);
+#pragma unroll 1
+                        for (int i = 0; i < kRounds - 1; ++i)
+                            if (row0 + i * kRowsPer >= own_from) odd |= clean(*reinterpret_cast<uint4*>(raw_gen + (kRounds + i) * 4096));
+                        return odd;
+                    };
                     auto store = [&](int which, char* base) {
                         const int c = (piece & 3) * 2;
                         char* const at0 = base + (piece >> 2) * S::kAtomBytes + row0 * 128 + ((c ^ (row0 & 7)) << 4);
@@ -703,6 +734,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             alive = warp_wait(&bars.v_empty[vi], ((at / S::kVStages) & 1u) ^ 1u);
                             if (!alive) break;
                             cp_async_wait<1>();
+                            const int own_from = w.a.r.start - (t0 + n) * kTcTile;
+                            const bool odd = kFmt == TL_KV_E4M3 && own_from < kTcTile && take_nan_out(own_from);
                             store(1, smem + S::kOffV + vi * S::kOperand);
                             float* const to = scales + vi * 3 * kTcTile + scale_row;
                             const float s_now = sc_lack ? 0.0f : sc;
@@ -715,6 +748,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             }
                             if (pt == 0) bars.meta[vi] = bad;
                             bad_any |= bad;
+                            const bool any_odd = kFmt == TL_KV_E4M3 && __any_sync(0xffffffffu, odd) != 0;
+                            if (kFmt == TL_KV_E4M3 && lane == 0) bars.odd[vi][warp - kTcProducerWarp] = any_odd;
                             fence_proxy_async_smem();
                             __syncwarp();
                             if (lane == 0) mbar_arrive(&bars.v_full[vi]);
