@@ -552,6 +552,8 @@ int tl_tree_mask(const int32_t* d_parents, const int32_t* d_token_offsets, int r
  * those whose bit is set in d_mask[i] (d_mask NULL: tokens 0 .. i of the request, a causal chain; one token per
  * request is ordinary decoding).  A token past the mask's words is not seen.  A row that sees nothing gives zeros
  * and lse = -infinity.  What a masked position holds (infinity, NaN, never written) has no influence.
+ * Over an 8-bit cache a value's scale below 2^-90 counts as 2^-90 (rows whose largest value is below 3.6e-25 in E4M3, 1.0e-25
+ * in INT8, are taken as larger than they are, by 2^-90 / scale; rows of zeros are zeros).
  *   d_q, d_out  bf16 [tokens][q_heads][head_dim], rows q_stride / out_stride elements apart, heads contiguous;
  *               pointers and strides multiples of 16 bytes.
  *   q_heads     a multiple of cache->heads.

@@ -295,9 +295,9 @@ attend_kernel(const AttendParams p) {
                     for (int nt = 0; nt < 2; ++nt) {
                         const float2 ks = *reinterpret_cast<const float2*>(sc + nt * 8 + 2 * t);
                         const float2 vs = *reinterpret_cast<const float2*>(sc + 16 + nt * 8 + 2 * t);
-                        // A row of zero values has scale 0: a tiny one in its place gives it its share of the sum.  A NaN
+                        // A row of zero values has scale 0: the floor in its place gives it its share of the sum.  A NaN
                         // scale reaches the score alone (the product with 0), which a mask can still replace.
-                        const float v0 = vs.x >= 1e-30f ? vs.x : 1e-30f, v1 = vs.y >= 1e-30f ? vs.y : 1e-30f;
+                        const float v0 = vs.x >= kScaleFloor ? vs.x : kScaleFloor, v1 = vs.y >= kScaleFloor ? vs.y : kScaleFloor;
                         const float lv0 = fmaf(vs.x, 0.0f, lg2(v0)), lv1 = fmaf(vs.y, 0.0f, lg2(v1));
                         rvs[u][nt][0] = __fdividef(1.0f, v0);
                         rvs[u][nt][1] = __fdividef(1.0f, v1);

@@ -742,7 +742,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             if (scale_of == 0) {
                                 to[0] = s_now;
                             } else {
-                                const float v = s_now >= 1e-30f ? s_now : 1e-30f;    // a row of zero values keeps its weight in the sum
+                                const float v = s_now >= kScaleFloor ? s_now : kScaleFloor;    // a row of zero values keeps its weight in the sum
                                 to[kTcTile] = fmaf(s_now, 0.0f, lg2(v));             // a NaN scale reaches the score alone
                                 to[2 * kTcTile] = __fdividef(1.0f, v);
                             }
