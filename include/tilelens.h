@@ -558,7 +558,8 @@ int tl_tree_mask(const int32_t* d_parents, const int32_t* d_token_offsets, int r
  *               pointers and strides multiples of 16 bytes.
  *   q_heads     a multiple of cache->heads.
  *   d_lse       NULL, or fp32 [tokens][q_heads]: natural logarithm of the sum of exp(scale * q . k).
- * Scores, softmax statistics and sums are fp32.  Scratch for sequences that several CTAs share comes from the
+ * Scores, softmax statistics and sums are fp32.  Over an 8-bit cache a weight, times its value's scale, enters the product with
+ * the values in f16: rounded to 11 bits, and to a multiple of 2^-31 of the row's largest such product.  Scratch for sequences that several CTAs share comes from the
  * workspace (tl_tree_attention_workspace_bytes; tl_set_workspace or the internal one).  A batch whose table and rows allow
  * 2^31 tiles or more is refused (TL_ERR_UNSUPPORTED).  Waits inside the kernel are bounded (TL_OPT_WAIT_LIMIT_US; detail
  * 0xc00 when one runs out).  Asynchronous.

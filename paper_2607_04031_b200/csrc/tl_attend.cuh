@@ -31,9 +31,16 @@ struct AttendParams {
     uint32_t* status;
 };
 
-// 8-bit caches: the least scale of a value.  Its reciprocal enters the sum of the weights, which 2^29 rows at the floor do not
-// overflow (weights are at most 2^8).  Weights of their own for smaller scales (a branch behind the exponentials, one more vote of
-// the producers) were measured: 1 to 2 % of every call with an 8-bit cache.
+// A row's weights are taken against a reference that stands for its maximum: a new one is taken when a score exceeds it by more than
+// kLag + attend_head (log2), attend_head below the score.  With 8-bit caches the weight (times the value's scale) enters the second product in
+// f16: at most 2^15 and, of the largest, 2^7 at least, it has all of f16's exponents, and one that is subnormal is off by 2^-32 of
+// the largest.  bf16 has fp32's exponents: the maximum itself.
+constexpr float kLag = 8.0f;
+__host__ __device__ constexpr float attend_head(int format) { return format == TL_KV_BF16 ? 0.0f : 7.0f; }
+
+// 8-bit caches: the least scale of a value.  Its reciprocal enters the sum of the weights, which has room for 2^22 rows at the floor
+// whose weights are all 2^15 (2^30 of 2^7).  Weights of their own for smaller scales (a branch behind the exponentials, one more vote
+// of the producers) were measured: 1 to 2 % of every call with an 8-bit cache.
 constexpr float kScaleFloor = 0x1p-90f;
 
 #ifdef __CUDACC__

@@ -13,8 +13,8 @@
 //   p v:   codes of two tokens at the same dimensions, interleaved bytewise, are one fragment pair each.
 // 8-bit codes become f16 (exact for both formats), q becomes f16 scaled by a power of two per row (exact but for
 // elements 2^-31 below the row's largest).  The key's scale multiplies the score.  The value's scale goes into the
-// exponent, w_j = 2^(s_j + log2 vs_j - m), with m the running maximum of s_j + log2 vs_j: w is at most 1 and as exact
-// as f16 can be where the contribution w_j v_j is large, and the softmax sum is that of w_j / vs_j.  The second product
+// exponent, w_j = 2^(s_j + log2 vs_j - m), with m following the maximum of s_j + log2 vs_j (attend_head): w is as exact as f16
+// can be where the contribution w_j v_j is large, and the softmax sum is that of w_j / vs_j.  The second product
 // takes w rounded to f16 (11 bits) with 8-bit caches, and as two bf16 terms (16 bits) with bf16 caches, whose eight bits
 // alone would put as much error into the result as its own rounding does; the sum takes w in fp32.
 //
@@ -34,6 +34,7 @@ template <int kDim, int kFmt, int kMT>
 struct SmallShape {
     static constexpr bool kBf16 = kFmt == TL_KV_BF16;
     static constexpr int kItem = kBf16 ? 2 : 1;
+    static constexpr float kHead = attend_head(kFmt);
     static constexpr int kRowBytes = kDim * kItem;
     static constexpr int kCtasPerSm = kMT == 1 && kRowBytes == 128 ? 3 : kMT == 1 && kRowBytes < 128 ? 2 : 1;
     static constexpr int kWarps = kDim == 256 || kCtasPerSm == 3 ? 4 : 8;
@@ -344,8 +345,8 @@ attend_kernel(const AttendParams p) {
                     if (!kBf16 && !here[u]) rvs[u][0][0] = rvs[u][0][1] = rvs[u][1][0] = rvs[u][1][1] = 0.0f;   // (never loaded)
                 }
             }
-            // The maximum may lag by up to 2^8: weights are at most 256 then, which f16 and the sums have room for, and the
-            // rescaling of O, half of all turns with an exact maximum, becomes rare.
+            // The reference may lag by up to 2^8, which f16 and the sums have room for: the rescaling of O, half of all turns with an
+            // exact maximum, becomes rare.
             float top[kMT][2];
             bool grew = false;
 #pragma unroll
@@ -357,7 +358,7 @@ attend_kernel(const AttendParams p) {
                     for (int u = 0; u < S::kSub; ++u)
                         x = fmaxf(x, fmaxf(fmaxf(s[u][mt][0][2 * h], s[u][mt][0][2 * h + 1]), fmaxf(s[u][mt][1][2 * h], s[u][mt][1][2 * h + 1])));
                     top[mt][h] = x;
-                    grew |= x > m[mt][h] + 8.0f;
+                    grew |= x > m[mt][h] + (kLag + S::kHead);
                 }
             if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
@@ -367,9 +368,9 @@ attend_kernel(const AttendParams p) {
                         float x = fmaxf(top[mt][h], __shfl_xor_sync(0xffffffffu, top[mt][h], 1));
                         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
                         // (by the row's own scores: what other rows see leaves its bits alone)
-                        const bool up = x > m[mt][h] + 8.0f;
-                        const float f = up ? ex2(m[mt][h] - x) : 1.0f;
-                        m[mt][h] = up ? x : m[mt][h];
+                        const bool up = x > m[mt][h] + (kLag + S::kHead);
+                        const float to = x - S::kHead, f = up ? ex2(m[mt][h] - to) : 1.0f;
+                        m[mt][h] = up ? to : m[mt][h];
                         l[mt][h] *= f;
 #pragma unroll
                         for (int j = 0; j < S::kNTiles; ++j) {

@@ -11,10 +11,11 @@
 // shared memory, 128-byte swizzle), the warpgroup reads S, writes the weights back over it as 16-bit values, and O += P V
 // takes P from tensor memory and V from shared memory as an MN-major operand, so neither P nor V^T is ever laid out again.
 //
-// The row maximum is allowed to lag: weights are taken against the maximum known so far, and only when a score exceeds
-// it by more than 2^8 are O, the sum and the tile's earlier weights rescaled; sums are fp32 and f16 has room for 2^15, so
-// the lag costs no accuracy.  Rows are rescaled by their own scores alone: a row's bits do not depend on what its neighbours see.  Scales of 8-bit caches enter as in the kernel for few rows (key's
-// scale on the score, value's in the exponent), q is f16 scaled by a power of two per row; conversion to f16 is exact.
+// A row's reference may lag behind its maximum (attend_head): only when a score exceeds it by more than 2^8 are O, the sum and the
+// tile's earlier weights rescaled; sums are fp32 and f16 has room for the weights, so the lag costs no accuracy.  Rows are
+// rescaled by their own scores alone: a row's bits do not depend on what its neighbours see.  Scales of 8-bit caches enter as
+// in the kernel for few rows (key's scale on the score, value's in the exponent), q is f16 scaled by a power of two per row;
+// conversion to f16 is exact.
 //
 // 8-bit tiles are fetched by the producers one tile ahead, converted and stored swizzled; full bf16 tiles
 // come by TMA (128-byte-swizzled boxes, one per page and 64 dimensions); a tile with positions past the end, or with a
@@ -169,6 +170,7 @@ template <int kDim, int kFmt, int kBlocks>
 __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_constant__ AttendTcParams tp) {
     using S = TcShape<kDim, kBlocks>;
     constexpr bool kBf16 = kFmt == TL_KV_BF16;
+    constexpr float kHead = attend_head(kFmt);
     extern __shared__ char smem_raw[];
     char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     TcBars& bars = *reinterpret_cast<TcBars*>(smem + S::kOffBar);
@@ -395,16 +397,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             top[h] = fmaxf(top[h], fmaxf(fmaxf(d[h][2].x, d[h][2].y), fmaxf(d[h][3].x, d[h][3].y)));
                             over = fmaxf(over, top[h] - m[h]);
                         }
-                        if (__any_sync(0xffffffffu, over > 8.0f)) {
+                        if (__any_sync(0xffffffffu, over > kLag + kHead)) {
                             // a new maximum: what was taken against the old one is rescaled
                             float f[4];
 #pragma unroll
                             for (int h = 0; h < 4; ++h) {
                                 top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
                                 top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
-                                const bool up = top[h] > m[h] + 8.0f;        // (by the row's own scores)
-                                f[h] = up ? ex2(m[h] - top[h]) : 1.0f;
-                                m[h] = up ? top[h] : m[h];
+                                const bool up = top[h] > m[h] + (kLag + kHead);        // (by the row's own scores)
+                                f[h] = up ? ex2(m[h] - (top[h] - kHead)) : 1.0f;
+                                m[h] = up ? top[h] - kHead : m[h];
                                 l[h] *= f[h];
                                 sum[h] = f2_mul(sum[h], F2{f[h], f[h]});
                             }
