@@ -582,7 +582,9 @@ size_t tl_tree_attention_workspace_bytes(const tl_kv_cache* cache, const tl_kv_b
  * From the root on: let r = p (the node's row of d_target), q its row of d_draft, S = 1.  Its children, in index order:
  * child c with token x is kept when accept[c] * q(x) * S < r(x), and the walk goes on from it; else
  * r = max(r - S q, 0), S = sum of r, and the next child is tried (if S is then 0: r = p, and no further child is
- * tried).  Without d_draft q is 1 at x and 0 elsewhere, r(x) becomes 0 and S becomes S - min(r(x), S).  Where no child
+ * tried).  Of one node's children the first 512 are tried; the others are as if they were not there (the tokens are
+ * distributed as the target's own all the same).  Without d_draft q is 1 at x and 0 elsewhere, r(x) becomes 0 and S
+ * becomes S - min(r(x), S).  Where no child
  * is kept the next token is drawn from r: the first id whose running sum of r exceeds sample[b] * (sum of r) (the last
  * id with r > 0 at most; r = p if r is empty; -1 if p is too).  Kept tokens and the drawn one are then distributed as
  * the target's own.  Probabilities that are negative or NaN, and ids outside [0, vocab), count as zero.  Sums over the

@@ -62,10 +62,6 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) tree_verify_kernel(const Ve
     pdl_launch_dependents();
     const int rank = int(blockIdx.x) % cluster, b = int(blockIdx.x) / cluster;
     const int lane = int(lane_id()), warp = threadIdx.x / 32;
-    KvBatchView bv = {};
-    bv.offsets = p.offsets;
-    bv.requests = p.requests;
-    bv.tokens = p.rows;
     const int first = min(max(p.offsets[b], 0), p.rows);
     const int n = min(max(p.offsets[b + 1], first), p.rows) - first;
     if (n == 0) {                                            // (the same for the whole cluster)
@@ -233,10 +229,11 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) tree_verify_kernel(const Ve
                     gather(c, node, token, pc, qc);
                 }
                 const double r = value(token, pc, qc), q = positive(qc);
-                if (double(u) * q * mass < r) {
+                if (tries < kVerifyTries && double(u) * q * mass < r) {
                     next = c;
                     break;
                 }
+                // (what is not tried can neither be kept nor changes the residual)
                 if (tries == kVerifyTries) {
                     open = false;
                     break;
