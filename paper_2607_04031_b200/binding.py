@@ -467,6 +467,7 @@ class KvBatch(ctypes.Structure):
     """tl_kv_batch; keeps the tensors it was made from alive."""
     _fields_ = [("page_table", _vp), ("start", _vp), ("token_offsets", _vp), ("table_stride", _i64),
                 ("requests", ctypes.c_int32), ("tokens", ctypes.c_int32)]
+    _device = None                                           # of the tensors, where it was made from some
 
 
 def _cuda(t: torch.Tensor, name: str, dtype=None, dims=None) -> torch.Tensor:
@@ -479,8 +480,14 @@ def _cuda(t: torch.Tensor, name: str, dtype=None, dims=None) -> torch.Tensor:
     return t
 
 
-def _int32(t: torch.Tensor, name: str, shape) -> int:
-    if t.dtype is not torch.int32 or not t.is_cuda or t.shape != shape or not t.is_contiguous():
+def _elsewhere(t: torch.Tensor, name: str, device: int) -> ValueError:
+    return ValueError(f"{name}: expected a tensor on cuda:{device}, got {'cuda:%d' % t.get_device() if t.is_cuda else 'the CPU'}")
+
+
+def _int32(t: torch.Tensor, name: str, shape, device: int) -> int:
+    if t.dtype is not torch.int32 or t.get_device() != device or t.shape != shape or not t.is_contiguous():
+        if t.is_cuda and t.get_device() != device:
+            raise _elsewhere(t, name, device)
         raise ValueError(f"{name}: expected a contiguous CUDA tensor of int32 and shape {tuple(shape)}, got {t.dtype}, {tuple(t.shape)}")
     return t.data_ptr()
 
@@ -509,7 +516,10 @@ def kv_cache(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = No
         c.scale_page_stride, c.scale_head_stride = k_scale.stride()[:2]
     elif k_scale is not None or v_scale is not None:
         raise ValueError("a bf16 cache has no scales")
-    c._tensors, c._ref, c._device = (k, v, k_scale, v_scale), ctypes.byref(c), k.device.index
+    c._tensors, c._ref, c._device = (k, v, k_scale, v_scale), ctypes.byref(c), k.get_device()
+    for t, name in ((v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale")):
+        if t is not None and t.get_device() != c._device:
+            raise _elsewhere(t, name, c._device)
     return c
 
 
@@ -518,9 +528,10 @@ def kv_batch(page_table: torch.Tensor, start: torch.Tensor, token_offsets: torch
     _cuda(page_table, "page_table", torch.int32, 2)
     n = page_table.shape[0]
     b = KvBatch()
-    b.page_table = _int32(page_table, "page_table", page_table.shape)
-    b.start = _int32(start, "start", (n,))
-    b.token_offsets = _int32(token_offsets, "token_offsets", (n + 1,))
+    b._device = device = page_table.get_device()
+    b.page_table = _int32(page_table, "page_table", page_table.shape, device)
+    b.start = _int32(start, "start", (n,), device)
+    b.token_offsets = _int32(token_offsets, "token_offsets", (n + 1,), device)
     b.table_stride = page_table.shape[1]
     b.requests, b.tokens = n, int(tokens)
     b._tensors, b._ref = (page_table, start, token_offsets), ctypes.byref(b)
@@ -530,8 +541,20 @@ def kv_batch(page_table: torch.Tensor, start: torch.Tensor, token_offsets: torch
 # The calls below run once per layer and step, next to kernels of a few microseconds: their checks read every attribute
 # once and build nothing that is not needed.
 
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
 def _kv_raw_stream(stream, device: int) -> int:
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    """The stream's handle.  The library launches on the current device, which has to be the tensors'."""
+    if stream is not None:
+        return stream.cuda_stream
+    if _current_device() != device:
+        raise ValueError(f"the tensors lie on cuda:{device}, the current device is cuda:{_current_device()}")
+    return _current_stream(device)
+
+
+def _apart(cache: KvCache, batch: KvBatch) -> ValueError:
+    return ValueError(f"the batch lies on cuda:{batch._device}, the cache on cuda:{cache._device}")
 
 
 def _kv_pair(k, v, cache, batch):
@@ -539,8 +562,13 @@ def _kv_pair(k, v, cache, batch):
     shape, stride, dtype = k.shape, k.stride(), k.dtype
     if v.shape != shape or v.stride() != stride or v.dtype is not dtype:
         raise ValueError("k and v: expected one shape, one element type and one set of strides")
-    if dtype not in _ELEMS or not (k.is_cuda and v.is_cuda):
+    if dtype not in _ELEMS:
         raise ValueError(f"k, v: expected CUDA tensors of bf16 or fp32, got {dtype}")
+    device = cache._device
+    if batch._device != device and batch._device is not None:
+        raise _apart(cache, batch)
+    if k.get_device() != device or v.get_device() != device:
+        raise _elsewhere(*((v, "v") if k.get_device() == device else (k, "k")), device)
     tokens, heads, dim = batch.tokens, cache.heads, cache.head_dim
     if shape != (tokens, heads, dim) or stride[2] != 1 or (heads > 1 and stride[1] != dim):
         raise ValueError("k, v: expected [tokens, heads, head_dim] with contiguous heads")
@@ -570,10 +598,13 @@ def kv_commit(cache: KvCache, batch: KvBatch, accepted: torch.Tensor, n_accepted
     shape, n = accepted.shape, batch.requests
     if len(shape) != 2:
         raise ValueError("accepted: expected [requests, n]")
-    a = _int32(accepted, "accepted", (n, shape[1]))
-    st = lib().tl_kv_commit(cache._ref, batch._ref, a, shape[1], _int32(n_accepted, "n_accepted", (n,)),
-                            _int32(new_start, "new_start", (n,)) if new_start is not None else None,
-                            _kv_raw_stream(stream, cache._device))
+    device = cache._device
+    if batch._device != device and batch._device is not None:
+        raise _apart(cache, batch)
+    a = _int32(accepted, "accepted", (n, shape[1]), device)
+    st = lib().tl_kv_commit(cache._ref, batch._ref, a, shape[1], _int32(n_accepted, "n_accepted", (n,), device),
+                            _int32(new_start, "new_start", (n,), device) if new_start is not None else None,
+                            _kv_raw_stream(stream, device))
     if st:
         _check(st, "tl_kv_commit")
 
@@ -581,10 +612,11 @@ def kv_commit(cache: KvCache, batch: KvBatch, accepted: torch.Tensor, n_accepted
 def tree_mask(parents: torch.Tensor, token_offsets: torch.Tensor, mask: torch.Tensor, stream=None):
     """mask (int32 [tokens, words]): bit j of row i is set when token i of its request sees token j."""
     _cuda(mask, "mask", torch.int32, 2)
-    m = _int32(mask, "mask", (parents.shape[0], mask.shape[1]))
-    _check(lib().tl_tree_mask(_int32(parents, "parents", (mask.shape[0],)),
-                              _int32(token_offsets, "token_offsets", (token_offsets.shape[0],)), token_offsets.shape[0] - 1,
-                              mask.shape[0], m, mask.shape[1], _kv_raw_stream(stream, mask.device.index)), "tl_tree_mask")
+    device = mask.get_device()
+    m = _int32(mask, "mask", (parents.shape[0], mask.shape[1]), device)
+    _check(lib().tl_tree_mask(_int32(parents, "parents", (mask.shape[0],), device),
+                              _int32(token_offsets, "token_offsets", (token_offsets.shape[0],), device), token_offsets.shape[0] - 1,
+                              mask.shape[0], m, mask.shape[1], _kv_raw_stream(stream, device)), "tl_tree_mask")
 
 
 def tree_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, out: torch.Tensor, mask: torch.Tensor | None = None,
@@ -594,23 +626,30 @@ def tree_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, out: torch.T
     [tokens, q_heads].  Rows of q and out may be strided."""
     shape, qs, os_ = q.shape, q.stride(), out.stride()
     tokens, dim = batch.tokens, cache.head_dim
-    if q.dtype is not torch.bfloat16 or out.dtype is not torch.bfloat16 or not (q.is_cuda and out.is_cuda):
+    if q.dtype is not torch.bfloat16 or out.dtype is not torch.bfloat16:
         raise ValueError("q, out: expected CUDA tensors of bf16")
     if len(shape) != 3 or out.shape != shape or shape[0] != tokens or shape[2] != dim or qs[2] != 1 or os_[2] != 1 or \
             (shape[1] > 1 and (qs[1] != dim or os_[1] != dim)):
         raise ValueError("q, out: expected [tokens, q_heads, head_dim] with contiguous heads")
+    device = cache._device
+    if batch._device != device and batch._device is not None:
+        raise _apart(cache, batch)
+    if q.get_device() != device or out.get_device() != device:
+        raise _elsewhere(*((out, "out") if q.get_device() == device else (q, "q")), device)
     heads, words, m, l = shape[1], 0, None, None
     wide = heads * dim
     if mask is not None:
         words = mask.shape[1]
-        m = _int32(mask, "mask", (tokens, words))
+        m = _int32(mask, "mask", (tokens, words), device)
     if lse is not None:
         if _cuda(lse, "lse", torch.float32).shape != shape[:2] or not lse.is_contiguous():
             raise ValueError("lse: expected a contiguous [tokens, q_heads]")
+        if lse.get_device() != device:
+            raise _elsewhere(lse, "lse", device)
         l = lse.data_ptr()
     st = lib().tl_tree_attention(cache._ref, batch._ref, q.data_ptr(), qs[0] if tokens > 1 else wide, heads, m, words,
                                  dim ** -0.5 if scale is None else scale, out.data_ptr(), os_[0] if tokens > 1 else wide, l,
-                                 _kv_raw_stream(stream, cache._device))
+                                 _kv_raw_stream(stream, device))
     if st:
         _check(st, "tl_tree_attention")
 
@@ -633,19 +672,25 @@ def tree_verify(target: torch.Tensor, draft: torch.Tensor | None, tokens: torch.
     requests, most = token_offsets.shape[0] - 1, accepted.shape[1]
     if target.dtype is not f32 or not target.is_cuda or (ts[1] != 1 and vocab > 1):
         raise ValueError("target: expected a CUDA tensor of fp32 with contiguous rows")
+    device = target.get_device()
     dp = ds = 0
     if draft is not None:
         ds = draft.stride()
-        if draft.dtype is not f32 or not draft.is_cuda or draft.shape != shape or (ds[1] != 1 and vocab > 1):
+        if draft.dtype is not f32 or draft.shape != shape or (ds[1] != 1 and vocab > 1):
             raise ValueError("draft: expected target's shape, type and contiguous rows")
+        if draft.get_device() != device:
+            raise _elsewhere(draft, "draft", device)
         dp, ds = draft.data_ptr(), ds[0] if rows > 1 else vocab
     for t, name, n in ((accept, "accept", rows), (sample, "sample", requests)):
-        if t.dtype is not f32 or not t.is_cuda or t.shape != (n,) or not t.is_contiguous():
+        if t.dtype is not f32 or t.shape != (n,) or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous CUDA tensor of {n} fp32 numbers")
-    st = lib().tl_tree_verify(target.data_ptr(), ts[0] if rows > 1 else vocab, dp, ds, vocab, _int32(tokens, "tokens", (rows,)),
-                              _int32(parents, "parents", (rows,)), _int32(token_offsets, "token_offsets", (requests + 1,)),
-                              requests, rows, accept.data_ptr(), sample.data_ptr(),
-                              _int32(accepted, "accepted", (requests, most)), most, _int32(n_accepted, "n_accepted", (requests,)),
-                              _int32(next_token, "next_token", (requests,)), _kv_raw_stream(stream, target.device.index))
+        if t.get_device() != device:
+            raise _elsewhere(t, name, device)
+    st = lib().tl_tree_verify(target.data_ptr(), ts[0] if rows > 1 else vocab, dp, ds, vocab, _int32(tokens, "tokens", (rows,), device),
+                              _int32(parents, "parents", (rows,), device),
+                              _int32(token_offsets, "token_offsets", (requests + 1,), device), requests, rows, accept.data_ptr(),
+                              sample.data_ptr(), _int32(accepted, "accepted", (requests, most), device), most,
+                              _int32(n_accepted, "n_accepted", (requests,), device),
+                              _int32(next_token, "next_token", (requests,), device), _kv_raw_stream(stream, device))
     if st:
         _check(st, "tl_tree_verify")
