@@ -105,12 +105,16 @@ static auto attend_tc_of(int format) {
 //                                                    32 rows: 16 requests bf16 87 / 87, E4M3 77 / 71, 64 requests INT8 144 / 130
 //                                    head_dim 64     32 rows: 16 requests bf16 60 / 69, E4M3 48 / 60; one request equal
 //                                    (either)        64 rows: 16 requests bf16 146 / 93, E4M3 126 / 77
-//   blocks of 128 or 256 rows, us:   256 rows: 1 request bf16 42 / 54, 4 requests E4M3 56 / 63 (7 tiles per SM),
-//                                    8 requests bf16 95 / 85 (14 tiles per SM), 8 over 8000 140 / 118
-//                                    160 rows: 8 over 8000 E4M3 97 / 108; 192 rows: 110 / 110
+//   blocks of 128 or 256 rows, us:   256 rows, contexts of half the length to all of it:
+//                                    1 request over 4100 (1.8 tiles of 256 rows per SM) bf16 34 / 44, E4M3 36 / 42
+//                                    4 over 8000 (10.8) bf16 76 / 79, E4M3 73 / 76; 8 over 2000 (5.6) 65 / 68, 55 / 60
+//                                    8 over 3000 (8.3) 76 / 75, 72 / 71; 8 over 4100 (11.2) 91 / 83, 83 / 80
+//                                    16 over 2000 (10.9) 116 / 94, 92 / 91; 192 rows, 8 over 8000 (21.6) 124 / 103, 120 / 108
+//                                    160 rows, 8 over 8000 E4M3 97 / 108
 // Blocks of 256 fetch and convert every tile for two streams at once, but need rows to fill them and more than a few
-// tiles per SM to pay for the wider joins.
-constexpr int kBlockRowsFrom = 192, kBlockTilesFrom = 10;
+// tiles per SM to pay for the wider joins.  The lengths are on the device; what the host knows is that they fit the table's rows and,
+// pages being one request's alone, the pool: a table as wide as the longest sequence there may ever be says little.
+constexpr int kBlockRowsFrom = 192, kBlockTilesFrom = 8;
 static int attend_plan(const tl_kv_cache* cache, const tl_kv_batch* batch, int q_heads, AttendPlan* plan) {
     const int group = q_heads / cache->heads;
     const int64_t rows = ceil_div(batch->tokens, batch->requests) * group;
@@ -120,7 +124,8 @@ static int attend_plan(const tl_kv_cache* cache, const tl_kv_batch* batch, int q
     if (cache->head_dim <= 128 && rows > (cache->head_dim == 128 ? 24 : 32)) {
         plan->tile_tokens = 128;
         plan->ctas_per_sm = 1;
-        const double tiles256 = double(batch->requests) * cache->heads * double(ceil_div(rows, 256)) * double(ceil_div(room, 128));
+        const double positions = std::min(double(batch->requests) * double(room), double(cache->pages) * cache->page_tokens);
+        const double tiles256 = cache->heads * double(ceil_div(rows, 256)) * std::ceil(positions / 128);
         plan->mma_rows = rows >= kBlockRowsFrom && tiles256 >= double(kBlockTilesFrom * sms) ? 256 : 128;
     } else {
         plan->mma_rows = rows > 16 && cache->head_dim <= 128 ? 32 : 16;
