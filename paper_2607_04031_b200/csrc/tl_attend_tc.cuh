@@ -398,15 +398,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             over = fmaxf(over, top[h] - m[h]);
                         }
                         if (__any_sync(0xffffffffu, over > kLag + kHead)) {
-                            // a new maximum: what was taken against the old one is rescaled
+                            // A new reference: what was taken against the old one is rescaled, by a whole power of two, so that weights that
+                            // are rounded already are not rounded again.
                             float f[4];
 #pragma unroll
                             for (int h = 0; h < 4; ++h) {
                                 top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
                                 top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
                                 const bool up = top[h] > m[h] + (kLag + kHead);        // (by the row's own scores)
-                                f[h] = up ? ex2(m[h] - (top[h] - kHead)) : 1.0f;
-                                m[h] = up ? top[h] - kHead : m[h];
+                                const float to = floorf(top[h]) - kHead;
+                                f[h] = up ? ex2(m[h] - to) : 1.0f;
+                                m[h] = up ? to : m[h];
                                 l[h] *= f[h];
                                 sum[h] = f2_mul(sum[h], F2{f[h], f[h]});
                             }
