@@ -559,10 +559,12 @@ int tl_tree_mask(const int32_t* d_parents, const int32_t* d_token_offsets, int r
  *   q_heads     a multiple of cache->heads.
  *   d_lse       NULL, or fp32 [tokens][q_heads]: natural logarithm of the sum of exp(scale * q . k).
  * Scores, softmax statistics and sums are fp32.  Over an 8-bit cache a weight, times its value's scale, enters the product with
- * the values in f16: rounded to 11 bits, and to a multiple of 2^-31 of the row's largest such product.  Scratch for sequences that several CTAs share comes from the
- * workspace (tl_tree_attention_workspace_bytes; tl_set_workspace or the internal one).  A batch whose table and rows allow
- * 2^31 tiles or more is refused (TL_ERR_UNSUPPORTED).  Waits inside the kernel are bounded (TL_OPT_WAIT_LIMIT_US; detail
- * 0xc00 when one runs out).  Asynchronous.
+ * the values in f16: rounded to 11 bits, and to a multiple of 2^-31 of the row's largest such product.  Over a bf16 cache it has 16
+ * bits where the batch averages at most 24 query rows per key/value head (32 at head_dim 64; always at 256), 8 bits above that.
+ * Scratch for sequences that several CTAs share comes from the workspace (tl_tree_attention_workspace_bytes;
+ * tl_set_workspace or the internal one).  A batch whose table and rows allow 2^31 tiles or more is refused
+ * (TL_ERR_UNSUPPORTED).  Waits inside the kernel are bounded (TL_OPT_WAIT_LIMIT_US; detail 0xc00 when one runs out).
+ * Asynchronous.
  */
 int tl_tree_attention(const tl_kv_cache* cache, const tl_kv_batch* batch, const void* d_q, int64_t q_stride, int q_heads,
                       const uint32_t* d_mask, int mask_words, float scale, void* d_out, int64_t out_stride, float* d_lse,
