@@ -575,7 +575,8 @@ size_t tl_tree_attention_workspace_bytes(const tl_kv_cache* cache, const tl_kv_b
 /*
  * Verification of draft trees (a chain is a tree of single children) against the target's distribution, with given
  * random numbers.  Rows as in tl_kv_batch: request b owns rows token_offsets[b] .. token_offsets[b + 1] - 1, its row 0
- * is the tree's root (the last token that is certain), parents as in tl_tree_mask.
+ * is the tree's root (the last token that is certain), parents as in tl_tree_mask.  That they are the tree whose mask
+ * tl_tree_attention was given is up to the caller.
  *   d_target   fp32 [tokens][vocab], rows target_stride apart: the target's distribution after each row's token.
  *   d_draft    fp32 [tokens][vocab], rows draft_stride apart: the distribution that the children of a row were drawn
  *              from, independently; or NULL: the children were chosen without chance.

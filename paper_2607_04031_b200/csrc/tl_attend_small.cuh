@@ -19,7 +19,7 @@
 // alone would put as much error into the result as its own rounding does; the sum takes w in fp32.
 //
 // What bounds it: the floor is one reading of the cache.  32 requests of one token (8 rows a head) over 4100 positions, E4M3:
-// 60.6 us, 3.5 TB/s, 0.53 of a plain copy; every byte is read once, the issue slots are 36 % in use and DRAM 43 %: the chain
+// 61.2 us, 3.4 TB/s, 0.53 of a plain copy; every byte is read once, the issue slots are 37 % in use and DRAM 43 %: the chain
 // from scores over maximum and exponential to the second product, with the 12 warps per SM that its registers allow.
 #pragma once
 

@@ -26,11 +26,13 @@
 // terms here, hence a second product: 1.66e-3, and 354 us instead of 284 to 297 there, 90 instead of 83 us for 8 requests of 256
 // rows over 4100, 37 instead of 34 for 1.
 //
-// What bounds it: the floor is the larger of one reading of the cache and the two products.  8 trees of 32 over 8000 (256 rows
-// a head, E4M3): 111 us, 400 TFLOP/s; 1 tree of 64 over 100000 (512 rows, bf16): 312 to 324 us, 650 to 670 TFLOP/s; 48 trees of 16 over
-// 6000 (128 rows, INT8): 241 to 247 us, 2.0 TB/s.  A step of two streams takes some 5200 clocks: 3700 for the softmax of a stream,
-// bound by the latency of reading scores, exponentials and writing weights (the exponentials alone are 2048), 1500
-// from its last weight over the second product to the next scores; the tensor pipe is in use for 29 to 38 % of the time.
+// What bounds it: the floor is the larger of one reading of the cache and the two products.  1 tree of 64 over 100000 (512 rows,
+// bf16): 312 to 328 us, 640 to 670 TFLOP/s; a step of two streams takes some 5200 clocks, 3500 of them a stream's softmax (bound by
+// the latency of reading scores, exponentials and writing weights; the exponentials alone are 2048) and 1500 to 1700 from its last
+// weight over the second product to the next scores.  8 trees of 32 over 8000 (216 rows a head, E4M3): 112 us, 400 TFLOP/s;
+// 6300 to 6700 clocks a step, 30 % of a stream's time without scores and 6 % without values.  48 trees of 16 over 6000 (104 rows,
+// INT8): 241 to 247 us, 2.0 TB/s; 4250 clocks per tile of 128 rows, the streams without values for 39 % of their time while the
+// producers wait for 16 % of theirs: fetching and converting the codes bounds it.  Tensor pipe in use: 38, 28 and 25 % of the time.
 #pragma once
 
 #include "tl_attend.cuh"

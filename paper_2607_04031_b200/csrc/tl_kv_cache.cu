@@ -2,8 +2,9 @@
 //
 // All three are copies with a conversion on the way: a group of head_dim / 8 lanes owns one head's row of one token (16 bytes
 // of bf16 and 8 of codes per lane), so that every access of the group is one contiguous row.  8192 new rows of 8 heads x 128
-// appended as INT8 and 27000 read back, both from and to bf16: 46.5 us for 219 MB (4.7 TB/s, 0.72 of a plain copy).  The floor
-// is HBM; on the way there the conversions fill 63 % (append, with the row's maximum) and 71 % (read) of the issue slots.
+// appended as INT8 and 27000 read back, both from and to bf16: 46.6 us for 219 MB (4.7 TB/s, 0.72 of a plain copy).  The floor
+// is HBM.  Apart and cold: append 20.0 us for 50 MB, latency bound (issue slots 64 %, 44 % of the warps), read 29.4 us for 167 MB (issue
+// slots 71 %).
 #include "tl_kv.cuh"
 
 #include <algorithm>

@@ -11,8 +11,8 @@
 //
 // What bounds it: the bytes of the rows p and q at the node where the walk stops (8 V bytes), and for a single request
 // the chain of dependent loads (offsets, parents and tokens, gathered probabilities, row, part of the row).  32 trees of 16
-// over 128256 ids: 23 us (1.4 TB/s of those bytes; issue slots 29 % in use, the rest is waiting along the chain and at the
-// cluster's barriers); one chain of 5 over 32000: 9.5 us, a launch and that chain.
+// over 128256 ids: 22 to 24 us (1.4 TB/s of those bytes; issue slots 29 % in use, the rest is waiting along the chain and at the
+// cluster's barriers); one chain of 5 over 32000: 9.2 to 10.6 us, a launch and that chain.
 #include "tl_kv.cuh"
 
 #include <algorithm>
