@@ -466,12 +466,14 @@ attend_kernel(const AttendParams p) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
 #pragma unroll
-                            for (int q = 0; q < kWords; ++q) {
-                                const uint32_t bad = e4m3_nan_bytes(v[k][q]);
-                                v[k][q] &= ~bad;
-                                any |= bad;
-                            }
-                        if (any != 0) *nan_taken = 1.0f;
+                            for (int q = 0; q < kWords; ++q) any |= e4m3_nan_bits(v[k][q]);
+                        if (__builtin_expect(any != 0, 0)) {
+                            *nan_taken = 1.0f;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                                for (int q = 0; q < kWords; ++q) v[k][q] &= ~e4m3_nan_bytes(v[k][q]);
+                        }
                     }
 #pragma unroll
                     for (int q = 0; q < kWords; ++q) {
@@ -559,21 +561,6 @@ attend_kernel(const AttendParams p) {
                 const float4 v = *reinterpret_cast<const float4*>(join + (k * S::kRows + r) * kDim + d);
                 sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
             }
-            if (kFmt == TL_KV_E4M3 && *nan_taken != 0.0f) {
-                const int tok = (w.block * S::kRows + r) / p.group;
-                for (int pos = t0 * S::kTile; pos < min(len, t1 * S::kTile); ++pos) {
-                    if (!attend_sees(p, w.a.r.first + tok, tok, pos - start)) continue;
-                    const int page = table[pos >> p.cache.page_shift];
-                    if (page < 0 || page >= p.cache.pages) continue;
-                    const uint32_t bad = e4m3_nan_bytes(*reinterpret_cast<const uint32_t*>(
-                        v_head + int64_t(page) * p.cache.page_stride + int64_t(pos & pos_mask) * p.cache.token_stride + d));
-                    const float nan = __uint_as_float(0x7fc00000u);
-                    if (bad & 0xffu) sum.x = nan;
-                    if (bad & 0xff00u) sum.y = nan;
-                    if (bad & 0xff0000u) sum.z = nan;
-                    if (bad & 0xff000000u) sum.w = nan;
-                }
-            }
             if (whole) {
                 const int row = w.block * S::kRows + r, tok = row / p.group, hq = w.head * p.group + row % p.group;
                 const float ll = row_l[r], inv = ll == 0.0f ? 0.0f : 1.0f / ll;
@@ -583,6 +570,25 @@ attend_kernel(const AttendParams p) {
             } else {
                 *reinterpret_cast<float4*>(p.part + (int64_t(slot) * S::kRows + r) * kDim + d) = sum;
                 if (d == 0) p.part_ml[int64_t(slot) * S::kRows + r] = make_float2(row_m[r], row_l[r]);
+            }
+        }
+        if (kFmt == TL_KV_E4M3 && *nan_taken != 0.0f) {
+            // what the rows see of the NaN codes that were taken out, over what this thread has just written
+            for (int e = threadIdx.x; e < rows * (kDim / 4); e += S::kThreads) {
+                const int r = e / (kDim / 4), d = e % (kDim / 4) * 4, row = w.block * S::kRows + r, tok = row / p.group;
+                uint32_t bad = 0;
+                for (int pos = max(start & ~15, t0 * S::kTile); pos < min(len, t1 * S::kTile); ++pos) {   // (whole groups of 16)
+                    const int page = table[pos >> p.cache.page_shift];
+                    if (page < 0 || page >= p.cache.pages || !attend_sees(p, w.a.r.first + tok, tok, pos - start)) continue;
+                    bad |= e4m3_nan_bits(*reinterpret_cast<const uint32_t*>(v_head + int64_t(page) * p.cache.page_stride +
+                                                                            int64_t(pos & pos_mask) * p.cache.token_stride + d));
+                }
+#pragma unroll 1
+                for (int i = 0; i < 4; ++i) {
+                    if (!(bad >> (8 * i) & 0x80u)) continue;
+                    if (whole) p.out[int64_t(w.a.r.first + tok) * p.out_stride + int64_t(w.head * p.group + row % p.group) * kDim + d + i] = __ushort_as_bfloat16(0x7fff);
+                    else p.part[(int64_t(slot) * S::kRows + r) * kDim + d + i] = __uint_as_float(0x7fc00000u);
+                }
             }
         }
         x += t1 - t0;

@@ -557,23 +557,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                                 }
                             }
                         }
-                        if (kFmt == TL_KV_E4M3 && odd_all) {
-                            // NaN codes alike: which of this row's 32 dimensions see one
-                            uint32_t nan = 0;
-                            const int from = max(w.a.r.start, t0 * kTcTile), to = min(w.a.r.len, t1 * kTcTile);
-#pragma unroll 1
-                            for (int pos = from; pos < to; ++pos) {
-                                if (!attend_sees(p, w.a.r.first + tok, tok, pos - w.a.r.start)) continue;
-                                const int page = p.batch.page_table[int64_t(w.b) * p.batch.table_stride + (pos >> p.cache.page_shift)];
-                                if (page < 0 || page >= p.cache.pages) continue;
-                                const char* const codes = p.cache.base[1] + int64_t(page) * p.cache.page_stride + int64_t(w.head) * p.cache.head_stride +
-                                                          int64_t(pos & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride + c * 32;
-#pragma unroll 1
-                                for (int i = 0; i < 32; ++i) nan |= ((codes[i] & 0x7f) == 0x7f ? 1u : 0u) << i;
-                            }
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = nan >> i & 1u ? __uint_as_float(0x7fc00000u) : o[i];
-                        }
                         if (whole) {
                             uint4* dst = reinterpret_cast<uint4*>(p.out + int64_t(w.a.r.first + tok) * p.out_stride + int64_t(hq) * kDim + c * 32);
 #pragma unroll
@@ -584,6 +567,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             float4* dst = reinterpret_cast<float4*>(p.part + (slot * S::kRows + prow) * kDim + c * 32);
 #pragma unroll
                             for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        }
+                    }
+                    if (kFmt == TL_KV_E4M3 && odd_all && live) {
+                        // NaN codes alike: what this row sees of them, over what has just been written
+                        const int from = max(w.a.r.start, t0 * kTcTile), to = min(w.a.r.len, t1 * kTcTile);
+#pragma unroll 1
+                        for (int pos = from; pos < to; ++pos) {
+                            if (!attend_sees(p, w.a.r.first + tok, tok, pos - w.a.r.start)) continue;
+                            const int page = p.batch.page_table[int64_t(w.b) * p.batch.table_stride + (pos >> p.cache.page_shift)];
+                            if (page < 0 || page >= p.cache.pages) continue;
+                            const char* const codes = p.cache.base[1] + int64_t(page) * p.cache.page_stride + int64_t(w.head) * p.cache.head_stride +
+                                                      int64_t(pos & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride;
+#pragma unroll 1
+                            for (int i = c_from * 32; i < c_to * 32; ++i) {
+                                if ((codes[i] & 0x7f) != 0x7f) continue;
+                                if (whole) p.out[int64_t(w.a.r.first + tok) * p.out_stride + int64_t(hq) * kDim + i] = __ushort_as_bfloat16(0x7fff);
+                                else p.part[(slot * S::kRows + prow) * kDim + i] = __uint_as_float(0x7fc00000u);
+                            }
                         }
                     }
                     if (live && c_from == 0) {
@@ -689,9 +690,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     // so an E4M3 NaN stays out of the product (a weight of 0 would not keep it out).  True: there was one.
                     auto take_nan_out = [&](int own_from) -> bool {
                         auto clean = [](uint4& v) -> bool {
-                            const uint4 bad = make_uint4(e4m3_nan_bytes(v.x), e4m3_nan_bytes(v.y), e4m3_nan_bytes(v.z), e4m3_nan_bytes(v.w));
-                            v = make_uint4(v.x & ~bad.x, v.y & ~bad.y, v.z & ~bad.z, v.w & ~bad.w);
-                            return (bad.x | bad.y | bad.z | bad.w) != 0;
+                            if (__builtin_expect((e4m3_nan_bits(v.x) | e4m3_nan_bits(v.y) | e4m3_nan_bits(v.z) | e4m3_nan_bits(v.w)) == 0, 1)) return false;
+                            v = make_uint4(v.x & ~e4m3_nan_bytes(v.x), v.y & ~e4m3_nan_bytes(v.y), v.z & ~e4m3_nan_bytes(v.z), v.w & ~e4m3_nan_bytes(v.w));
+                            return true;
                         };
                         bool odd = row0 + (kRounds - 1) * kRowsPer >= own_from && !lack && clean(last);
 #pragma unroll 1

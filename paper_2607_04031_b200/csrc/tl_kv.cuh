@@ -117,8 +117,10 @@ __device__ __forceinline__ void codes4_to_f16(uint32_t w, uint32_t& lo, uint32_t
     }
 }
 
-// The bytes that hold an E4M3 NaN (0x7f, 0xff), as a mask.  tl_kv_append writes none: they stand in memory that nobody wrote.
-__device__ __forceinline__ uint32_t e4m3_nan_bytes(uint32_t x) { return __vcmpeq4(x & 0x7f7f7f7fu, 0x7f7f7f7fu); }
+// Which bytes hold an E4M3 NaN (0x7f, 0xff): their top bits, and whole bytes.  tl_kv_append writes none: they stand in memory that
+// nobody wrote.
+__device__ __forceinline__ uint32_t e4m3_nan_bits(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ uint32_t e4m3_nan_bytes(uint32_t x) { return (e4m3_nan_bits(x) >> 7) * 0xffu; }
 
 // D (fp32 16 x 8) += A (16 x 16) B (16 x 8), operands f16 or bf16.
 template <bool kBf16>
