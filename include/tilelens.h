@@ -478,8 +478,15 @@ int tl_hw_box_load(const tl_hw_desc* desc, const void* d_src_tilemajor, uint64_t
  * (INT8) in fp32, code = x / scale (fp32) rounded to the nearest code, ties to even (the largest code at most: where the
  * scale is a subnormal number, x / scale may be larger).  The value held is code * scale.
  * A row of zeros has scale 0; a row with an infinity or a NaN has scale NaN and reads back as NaN.
+ * TL_KV_E2M1 holds 4-bit codes (a sign, two bits of exponent, one of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6; element 2i in the low half
+ * of byte i), one E4M3 byte per 16 elements and one fp32 scale per token and head: scale = the least power of two, 2^-126 at least,
+ * with 6 * 448 * scale >= a; group scale = (max |x| of the 16) / scale * c, c = 1/6 in fp32, rounded to E4M3, ties to even;
+ * code = x / (group scale * scale) rounded to the nearest, ties to even, 6 at most (0 under a group scale of 0).  The value held,
+ * code * group scale * scale, has at most 6 bits: it is exact in bf16.  A row that is all zeros has scale and group scales 0, a row
+ * with an infinity or a NaN has scale NaN.  Group scales in the memory of a page are read without their sign, 0x7f as 480, and row
+ * scales have to be below 2^118.
  */
-typedef enum { TL_KV_BF16 = 0, TL_KV_E4M3 = 1, TL_KV_INT8 = 2 } tl_kv_format;
+typedef enum { TL_KV_BF16 = 0, TL_KV_E4M3 = 1, TL_KV_INT8 = 2, TL_KV_E2M1 = 4 } tl_kv_format;
 typedef enum { TL_ELEM_BF16 = 0, TL_ELEM_F32 = 1 } tl_elem;
 
 typedef struct tl_kv_cache {
@@ -488,13 +495,16 @@ typedef struct tl_kv_cache {
     float* k_scale;             /* device, 16-byte aligned; NULL for TL_KV_BF16 */
     float* v_scale;
     int64_t pages;
-    int64_t page_stride, head_stride, token_stride;     /* elements, each a multiple of 16 bytes, a token's
-                                                           at most 2^26 bytes (else TL_ERR_UNSUPPORTED); all 0: packed */
+    int64_t page_stride, head_stride, token_stride;     /* elements (TL_KV_E2M1: two to a byte), each a multiple of 16 bytes, a
+                                                           token's at most 2^26 bytes (else TL_ERR_UNSUPPORTED); all 0: packed */
     int64_t scale_page_stride, scale_head_stride;       /* floats, multiples of 4; both 0: packed [page][head][token].
                                                            The scales of a page's tokens are contiguous. */
     int32_t format;             /* tl_kv_format */
     int32_t heads, head_dim;    /* head_dim 64, 128 or 256 */
     int32_t page_tokens;        /* power of two, 16 .. 1024 */
+    uint8_t* k_group;           /* TL_KV_E2M1 (the fields from here on are not read for other formats): device, 16-byte aligned, */
+    uint8_t* v_group;           /* [page][head][token][head_dim / 16], a head's tokens of a page contiguous */
+    int64_t group_page_stride, group_head_stride;       /* bytes, multiples of 16; both 0: packed */
 } tl_kv_cache;
 
 /*
@@ -553,12 +563,12 @@ int tl_tree_mask(const int32_t* d_parents, const int32_t* d_token_offsets, int r
  * request is ordinary decoding).  A token past the mask's words is not seen.  A row that sees nothing gives zeros
  * and lse = -infinity.  What a masked position holds (infinity, NaN, never written) has no influence.
  * Over an 8-bit cache a value's scale below 2^-90 counts as 2^-90 (rows whose largest value is below 3.6e-25 in E4M3, 1.0e-25
- * in INT8, are taken as larger than they are, by 2^-90 / scale; rows of zeros are zeros).
+ * in INT8, are taken as larger than they are, by 2^-90 / scale; rows of zeros are zeros); over a 4-bit one below 2^-98 as 2^-98.
  *   d_q, d_out  bf16 [tokens][q_heads][head_dim], rows q_stride / out_stride elements apart, heads contiguous;
  *               pointers and strides multiples of 16 bytes.
  *   q_heads     a multiple of cache->heads.
  *   d_lse       NULL, or fp32 [tokens][q_heads]: natural logarithm of the sum of exp(scale * q . k).
- * Scores, softmax statistics and sums are fp32.  Over an 8-bit cache a weight, times its value's scale, enters the product with
+ * Scores, softmax statistics and sums are fp32.  Over an 8-bit or 4-bit cache a weight, times its value's scale, enters the product with
  * the values in f16: rounded to 11 bits, and to a multiple of 2^-31 of the row's largest such product.  Over a bf16 cache it has 16
  * bits where the batch averages at most 24 query rows per key/value head (32 at head_dim 64; always at 256), 8 bits above that.
  * Scratch for sequences that several CTAs share comes from the workspace (tl_tree_attention_workspace_bytes;
@@ -601,6 +611,124 @@ int tl_tree_verify(const float* d_target, int64_t target_stride, const float* d_
                    const int32_t* d_tokens, const int32_t* d_parents, const int32_t* d_token_offsets, int requests,
                    int tokens, const float* d_accept, const float* d_sample, int32_t* d_accepted,
                    int64_t accepted_stride, int32_t* d_n_accepted, int32_t* d_next, void* cuda_stream);
+
+/* ------------------------------------------------------------------ rotary positions */
+
+/*
+ * Rotary positions: the first rotary_dim elements of a head's row are rotary_dim / 2 pairs, and pair i of the token at position t is
+ * turned by t times its frequency:  (x, y) -> amplitude * (x cos - y sin, y cos + x sin).  The other elements stay as they are.
+ * Pair i is (i, i + rotary_dim / 2) in TL_ROPE_HALF, (2i, 2i + 1) in TL_ROPE_INTERLEAVED.
+ *
+ * tl_rope_turns computes the frequencies once, on the host: base^(-2i / rotary_dim) radians per position, for long contexts
+ *   TL_ROPE_LINEAR  divided by factor;
+ *   TL_ROPE_BANDS   by wavelength: with n = original * frequency / 2 pi turns over the original context, divided by factor where
+ *                   n < low, left where n > high, blended between ((1 - u) / factor + u of it, u = (n - low) / (high - low));
+ *   TL_ROPE_RAMP    by pair number: left up to the pair that makes `high` turns over the original context, divided by factor from the
+ *                   one that makes `low`, blended between (the two rounded outwards and clamped to 0 .. rotary_dim - 1).
+ * h_turns (host, rotary_dim / 2) receives them in units of 2^-64 turns, so that position * h_turns modulo 2^64 is the angle of any
+ * int32 position with no error but the frequency's own rounding (2^-65 turns a position); the caller copies them to the device, where
+ * they serve every call.  An amplitude other than 1 (some scalings want one) is the caller's.
+ */
+typedef enum { TL_ROPE_HALF = 0, TL_ROPE_INTERLEAVED = 1 } tl_rope_layout;
+typedef enum { TL_ROPE_PLAIN = 0, TL_ROPE_LINEAR = 1, TL_ROPE_BANDS = 2, TL_ROPE_RAMP = 3 } tl_rope_scaling;
+int tl_rope_turns(int rotary_dim, double base, int scaling, double factor, double original, double low, double high,
+                  uint64_t* h_turns);
+
+typedef struct tl_rope {
+    const uint64_t* turns;      /* device, rotary_dim / 2; 8-byte aligned */
+    float amplitude;            /* finite */
+    int32_t rotary_dim;         /* even, 2 .. the rows' head_dim */
+    int32_t layout;             /* tl_rope_layout */
+} tl_rope;
+
+/*
+ * Turns rows: d_out[token][head] = the row d_x[token][head] at position d_positions[token] (device, int32, any sign).  inverse != 0
+ * turns the other way with the same amplitude, which is the transpose: it takes the gradient of d_out to that of d_x.
+ *   d_x, d_out  [tokens][heads][head_dim] of type elem, rows of a token x_stride / out_stride elements apart, heads contiguous;
+ *               d_out may be d_x (with its stride), and must not overlap it otherwise.  16-byte aligned rows (pointers, strides
+ *               and head_dim multiples of 16 bytes) with rotary_dim a multiple of 16 are moved in vectors, others by elements.
+ *   head_dim    even, at most 1024.
+ * fp32 arithmetic, angles as above; one rounding to elem.  Asynchronous.
+ */
+int tl_rope_rows(const tl_rope* rope, const void* d_x, int64_t x_stride, void* d_out, int64_t out_stride, int elem, int tokens,
+                 int heads, int head_dim, const int32_t* d_positions, int inverse, void* cuda_stream);
+/*
+ * A step's queries, keys and values in one kernel: d_q turned into d_q_out (bf16), keys turned and appended, values appended
+ * (tl_kv_append's rule; the turned keys enter it in fp32, without a rounding to elem).
+ *   d_positions  device int32 [tokens], or NULL: a row's position in its sequence, start[b] + i, is the one it is turned by.  (In a
+ *                draft tree that is start + depth: tl_tree_positions.)  A row's place in the cache is start[b] + i either way.
+ *   d_q          [tokens][q_heads][head_dim] of type elem, or NULL with q_heads 0.  d_q_out may be d_q if elem is bf16.
+ *   d_k, d_v     as in tl_kv_append.  Pointers and strides are multiples of 16 bytes.
+ * Queries of a row that no request owns, or that has no page, are turned all the same (by position 0 with d_positions NULL where no
+ * request owns it).  Asynchronous.
+ */
+int tl_rope_append(const tl_kv_cache* cache, const tl_kv_batch* batch, const tl_rope* rope, const int32_t* d_positions, const void* d_q,
+                   int64_t q_stride, int q_heads, void* d_q_out, int64_t q_out_stride, const void* d_k, const void* d_v, int elem,
+                   int64_t kv_stride, void* cuda_stream);
+/* Positions of draft trees: d_positions[row] = start[b] + the row's depth (0 for the root), parents as in tl_tree_mask.  Rows that no
+ * request owns are left alone.  Asynchronous. */
+int tl_tree_positions(const int32_t* d_parents, const int32_t* d_token_offsets, const int32_t* d_start, int requests, int tokens,
+                      int32_t* d_positions, void* cuda_stream);
+
+/* ------------------------------------------------------------------ pages */
+
+/*
+ * Whose pages are whose.  A set of tables over one pool: request b holds the pages page_table[b][0 .. held[b] - 1], and holders[p]
+ * counts the entries that name page p (0: the page is free).  Forked requests share pages; a page with several holders is not written.
+ * The calls below keep tables, held and holders consistent, on the device, in stream order; which page goes where depends on their
+ * contents alone.  Tables of one pool must not be worked on by two calls at once.  One table serves any number of caches of the same
+ * page count and page size (a model's layers): data moves in calls of its own, tl_page_copy, one per cache.
+ */
+typedef struct tl_page_tables {
+    int32_t* page_table;        /* device [requests][table_stride] */
+    int32_t* held;              /* device [requests], 0 .. table_stride */
+    int32_t* holders;           /* device [pages] */
+    int64_t table_stride;       /* >= 1, at most 2^30 */
+    int32_t requests, pages;    /* pages at most 2^30 */
+    int32_t page_tokens;        /* power of two, 16 .. 1024 */
+} tl_page_tables;
+
+/*
+ * Gives requests pages that they may write: afterwards request b holds pages for d_tokens[b] positions (it keeps what it holds beyond
+ * them), and those that hold the positions d_start[b] .. d_tokens[b] - 1 have no other holder.  A request with d_tokens[b] < 0 is left
+ * alone.  Entries that are missing, and entries in that range that others hold too, get fresh pages: the lowest free ones, in the order
+ * of requests and entries.  Where all holders of a page are to write it, the first of them (in that order) keeps it.  Of a replaced page
+ * the rows in front of d_start[b] are to be copied: d_moves ([requests][3]: from, to, rows) receives what tl_page_copy is to do, in the
+ * order of requests, *d_n_moves how many; entries behind those are left alone.
+ * If the free pages do not suffice nothing changes, *d_n_moves is 0 and *d_missing says how many more it takes; else it is 0.
+ * Positions past the table are left out and reported (tl_device_status, detail 0xa00).
+ * Scratch comes from the workspace (tl_page_workspace_bytes).  Asynchronous.
+ */
+int tl_page_reserve(const tl_page_tables* tables, const int32_t* d_start, const int32_t* d_tokens, int32_t* d_moves, int32_t* d_n_moves,
+                    int32_t* d_missing, void* cuda_stream);
+/* Gives pages back: request b keeps those of its first d_tokens[b] positions (all of them if d_tokens[b] < 0; d_tokens NULL: none of
+ * any request), the other entries become -1.  A page is free when its last holder lets go.  Asynchronous. */
+int tl_page_release(const tl_page_tables* tables, const int32_t* d_tokens, void* cuda_stream);
+/*
+ * Request d_to[f], which must hold nothing, comes to hold the pages of the first d_tokens[f] positions of request d_from[f] (as far as
+ * it holds them) together with it; no data moves.  All forks see the tables as they are before the call.  A fork to a request that holds
+ * pages, or that an earlier fork of the call goes to, or with a request outside the tables, is left out and reported (detail 0xd00).
+ * Asynchronous.
+ */
+int tl_page_fork(const tl_page_tables* tables, const int32_t* d_from, const int32_t* d_to, const int32_t* d_tokens, int forks,
+                 void* cuda_stream);
+/*
+ * Moves the pages in use to the front of the pool: the highest one in use to the lowest free place, and so on, as long as the place lies
+ * below the page, at most `most` of them.  d_moves ([most][3]: from, to, page_tokens) receives the moves for tl_page_copy, *d_n_moves
+ * how many, *d_in_use how many pages are in use (after all moves they are the pages below that number).  Tables and holders are
+ * those after the moves.  Every request with pages in the pool has to be in `tables`.  Asynchronous.
+ */
+int tl_page_compact(const tl_page_tables* tables, int32_t* d_moves, int most, int32_t* d_n_moves, int32_t* d_in_use, void* cuda_stream);
+/* Workspace of tl_page_reserve, tl_page_fork and tl_page_compact with these tables and `forks` forks (0 for arguments they refuse). */
+size_t tl_page_workspace_bytes(const tl_page_tables* tables, int forks);
+/*
+ * Copies pages: for i < *d_n_moves (d_n_moves NULL: most; never more than most) the first d_moves[i][2] tokens of page d_moves[i][0] of
+ * `from` (keys, values and scales as they are) to page d_moves[i][1] of `to`: the same cache, or another of the same format, heads,
+ * head_dim and page_tokens.  No page may be written twice, or both read and written, by one call.  A page number outside its pool is
+ * skipped and reported (detail 0xa00).  Asynchronous.
+ */
+int tl_page_copy(const tl_kv_cache* from, const tl_kv_cache* to, const int32_t* d_moves, const int32_t* d_n_moves, int most,
+                 void* cuda_stream);
 
 /* --------------------------------------------------- read amplification */
 

@@ -69,6 +69,16 @@ _SIGNATURES = {
     "tl_tree_attention": (_int, [_vp, _vp, _vp, _i64, _int, _vp, _int, ctypes.c_float, _vp, _i64, _vp, _vp]),
     "tl_tree_attention_workspace_bytes": (_sz, [_vp, _vp, _int]),
     "tl_tree_verify": (_int, [_vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _int, _int, _vp, _vp, _vp, _i64, _vp, _vp, _vp]),
+    "tl_rope_turns": (_int, [_int, ctypes.c_double, _int, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double, _vp]),
+    "tl_rope_rows": (_int, [_vp, _vp, _i64, _vp, _i64, _int, _int, _int, _int, _vp, _int, _vp]),
+    "tl_rope_append": (_int, [_vp, _vp, _vp, _vp, _vp, _i64, _int, _vp, _i64, _vp, _vp, _int, _i64, _vp]),
+    "tl_tree_positions": (_int, [_vp, _vp, _vp, _int, _int, _vp, _vp]),
+    "tl_page_reserve": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "tl_page_release": (_int, [_vp, _vp, _vp]),
+    "tl_page_fork": (_int, [_vp, _vp, _vp, _vp, _int, _vp]),
+    "tl_page_compact": (_int, [_vp, _vp, _int, _vp, _vp, _vp]),
+    "tl_page_workspace_bytes": (_sz, [_vp, _int]),
+    "tl_page_copy": (_int, [_vp, _vp, _vp, _vp, _int, _vp]),
     "tl_read_amp_per_cta": (_int, [_i64, _i64, _i64, _int, _int, _int, _int, _i64, _int, _int, _int, _vp, _vp, _vp]),
 }
 
@@ -449,9 +459,9 @@ def read_amp_per_cta(M: int, N: int, K: int, cta, layout: int, G: int, block_row
 
 # ------------------------------------------------------------------ key/value cache for drafted tokens
 
-KV_BF16, KV_E4M3, KV_INT8 = 0, 1, 2
+KV_BF16, KV_E4M3, KV_INT8, KV_E2M1 = 0, 1, 2, 4
 ELEM_BF16, ELEM_F32 = 0, 1
-_KV_FORMATS = {torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_E4M3, torch.int8: KV_INT8}
+_KV_FORMATS = {torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_E4M3, torch.int8: KV_INT8, torch.uint8: KV_E2M1}
 _ELEMS = {torch.bfloat16: ELEM_BF16, torch.float32: ELEM_F32}
 
 
@@ -460,7 +470,8 @@ class KvCache(ctypes.Structure):
     _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("pages", _i64), ("page_stride", _i64),
                 ("head_stride", _i64), ("token_stride", _i64), ("scale_page_stride", _i64), ("scale_head_stride", _i64),
                 ("format", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
-                ("page_tokens", ctypes.c_int32)]
+                ("page_tokens", ctypes.c_int32), ("k_group", _vp), ("v_group", _vp), ("group_page_stride", _i64),
+                ("group_head_stride", _i64)]
 
 
 class KvBatch(ctypes.Structure):
@@ -493,20 +504,24 @@ def _int32(t: torch.Tensor, name: str, shape, device: int) -> int:
 
 
 def kv_cache(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None,
-             v_scale: torch.Tensor | None = None) -> KvCache:
+             v_scale: torch.Tensor | None = None, k_group: torch.Tensor | None = None,
+             v_group: torch.Tensor | None = None) -> KvCache:
     """k, v: [pages, heads, page_tokens, head_dim], bf16, float8_e4m3fn or int8, the last dimension contiguous (the other
     strides are free: a permuted [pages, page_tokens, heads, head_dim] pool serves too).  k_scale, v_scale: fp32
-    [pages, heads, page_tokens], for the 8-bit formats."""
+    [pages, heads, page_tokens], for the 8-bit and 4-bit formats.  The 4-bit one: k, v uint8 [..., head_dim / 2], two E2M1 codes
+    a byte, and k_group, v_group float8_e4m3fn [pages, heads, page_tokens, head_dim / 16]."""
     _cuda(k, "k", dims=4), _cuda(v, "v", k.dtype, 4)
     if k.dtype not in _KV_FORMATS:
-        raise ValueError(f"k: expected bf16, float8_e4m3fn or int8, got {k.dtype}")
+        raise ValueError(f"k: expected bf16, float8_e4m3fn, int8 or (4 bits) uint8, got {k.dtype}")
     if v.shape != k.shape or v.stride() != k.stride() or k.stride(3) != 1:
         raise ValueError("k and v: expected one shape and one set of strides, the last dimension contiguous")
     c = KvCache()
     c.format = _KV_FORMATS[k.dtype]
+    two = 2 if c.format == KV_E2M1 else 1                    # elements to one of the tensors'
     c.pages, c.heads, c.page_tokens, c.head_dim = k.shape
+    c.head_dim *= two
     c.k, c.v = k.data_ptr(), v.data_ptr()
-    c.page_stride, c.head_stride, c.token_stride = k.stride()[:3]
+    c.page_stride, c.head_stride, c.token_stride = (n * two for n in k.stride()[:3])
     if c.format != KV_BF16:
         for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
             _cuda(t, name, torch.float32, 3)
@@ -516,8 +531,18 @@ def kv_cache(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = No
         c.scale_page_stride, c.scale_head_stride = k_scale.stride()[:2]
     elif k_scale is not None or v_scale is not None:
         raise ValueError("a bf16 cache has no scales")
-    c._tensors, c._ref, c._device = (k, v, k_scale, v_scale), ctypes.byref(c), k.get_device()
-    for t, name in ((v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale")):
+    if c.format == KV_E2M1:
+        n = c.head_dim // 16
+        for t, name in ((k_group, "k_group"), (v_group, "v_group")):
+            _cuda(t, name, torch.float8_e4m3fn, 4)
+            if tuple(t.shape) != (*k.shape[:3], n) or t.stride() != k_group.stride() or t.stride()[2:] != (n, 1):
+                raise ValueError(f"{name}: expected [pages, heads, page_tokens, head_dim / 16], a head's tokens contiguous, one set of strides")
+        c.k_group, c.v_group = k_group.data_ptr(), v_group.data_ptr()
+        c.group_page_stride, c.group_head_stride = k_group.stride()[:2]
+    elif k_group is not None or v_group is not None:
+        raise ValueError("only a 4-bit cache has group scales")
+    c._tensors, c._ref, c._device = (k, v, k_scale, v_scale, k_group, v_group), ctypes.byref(c), k.get_device()
+    for t, name in ((v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale"), (k_group, "k_group"), (v_group, "v_group")):
         if t is not None and t.get_device() != c._device:
             raise _elsewhere(t, name, c._device)
     return c
@@ -694,3 +719,184 @@ def tree_verify(target: torch.Tensor, draft: torch.Tensor | None, tokens: torch.
                               _int32(next_token, "next_token", (requests,), device), _kv_raw_stream(stream, device))
     if st:
         _check(st, "tl_tree_verify")
+
+
+# ------------------------------------------------------------------ rotary positions
+
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3
+
+
+class Rope(ctypes.Structure):
+    """tl_rope; keeps the tensor it was made from alive."""
+    _fields_ = [("turns", _vp), ("amplitude", ctypes.c_float), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32)]
+
+
+def rope_turns(rotary_dim: int, base: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0, original: float = 0.0,
+               low: float = 1.0, high: float = 4.0) -> torch.Tensor:
+    """The frequencies of a model's rotary positions, int64 [rotary_dim / 2] on the host (2^-64 turns per position): computed once
+    and copied to the device.  low and high: turns over the original context (ROPE_BANDS usually 1 and 4, ROPE_RAMP 1 and 32)."""
+    out = torch.empty(max(0, rotary_dim // 2), dtype=torch.int64)
+    _check(lib().tl_rope_turns(rotary_dim, base, scaling, factor, original, low, high, out.data_ptr()), "tl_rope_turns")
+    return out
+
+
+def rope(turns: torch.Tensor, layout: int = ROPE_HALF, amplitude: float = 1.0) -> Rope:
+    """turns: what rope_turns gave, on the device."""
+    _cuda(turns, "turns", torch.int64, 1)
+    if not turns.is_contiguous():
+        raise ValueError("turns: expected a contiguous tensor")
+    r = Rope()
+    r.turns, r.amplitude, r.rotary_dim, r.layout = turns.data_ptr(), amplitude, 2 * turns.shape[0], layout
+    r._tensors, r._ref, r._device = (turns,), ctypes.byref(r), turns.get_device()
+    return r
+
+
+def _head_rows(t: torch.Tensor, name: str, shape, device: int):
+    """Stride between the tokens of a [tokens, heads, head_dim] tensor with contiguous heads."""
+    stride = t.stride()
+    if t.shape != shape or (shape[2] > 1 and stride[2] != 1) or (shape[1] > 1 and stride[1] != shape[2]):
+        raise ValueError(f"{name}: expected {tuple(shape)} with contiguous heads, got {tuple(t.shape)}")
+    if t.get_device() != device:
+        raise _elsewhere(t, name, device)
+    return stride[0] if shape[0] > 1 else shape[1] * shape[2]
+
+
+def rope_rows(rope: Rope, x: torch.Tensor, out: torch.Tensor, positions: torch.Tensor, inverse: bool = False, stream=None):
+    """out = x [tokens, heads, head_dim] (bf16 or fp32; out may be x) turned by positions (int32 [tokens]); inverse: turned back, the
+    gradient of x from that of out."""
+    shape, device = x.shape, rope._device
+    if x.dtype not in _ELEMS or out.dtype is not x.dtype:
+        raise ValueError(f"x, out: expected CUDA tensors of bf16 or of fp32, got {x.dtype} and {out.dtype}")
+    if len(shape) != 3:
+        raise ValueError("x: expected [tokens, heads, head_dim]")
+    xs, os_ = _head_rows(x, "x", shape, device), _head_rows(out, "out", shape, device)
+    st = lib().tl_rope_rows(rope._ref, x.data_ptr(), xs, out.data_ptr(), os_, _ELEMS[x.dtype], shape[0], shape[1], shape[2],
+                            _int32(positions, "positions", (shape[0],), device), 1 if inverse else 0, _kv_raw_stream(stream, device))
+    if st:
+        _check(st, "tl_rope_rows")
+
+
+def rope_append(cache: KvCache, batch: KvBatch, rope: Rope, q: torch.Tensor | None, q_out: torch.Tensor | None, k: torch.Tensor,
+                v: torch.Tensor, positions: torch.Tensor | None = None, stream=None):
+    """q ([tokens, q_heads, head_dim], k's type; None: keys and values alone) turned into q_out (bf16), k turned and appended, v appended.
+    positions: int32 [tokens] (None: every row's position in its sequence; in a draft tree tree_positions gives them)."""
+    kp, vp, elem, stride = _kv_pair(k, v, cache, batch)
+    device = cache._device
+    if rope._device != device:
+        raise ValueError(f"the frequencies lie on cuda:{rope._device}, the cache on cuda:{device}")
+    qp = op = None
+    heads = qs = os_ = 0
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out: expected both or neither")
+    if q is not None:
+        if q.dtype is not k.dtype or q_out.dtype is not torch.bfloat16:
+            raise ValueError(f"q: expected {k.dtype}, q_out: expected bf16, got {q.dtype} and {q_out.dtype}")
+        if len(q.shape) != 3:
+            raise ValueError("q: expected [tokens, q_heads, head_dim]")
+        shape = (batch.tokens, q.shape[1], cache.head_dim)
+        qs, os_ = _head_rows(q, "q", shape, device), _head_rows(q_out, "q_out", shape, device)
+        heads, qp, op = shape[1], q.data_ptr(), q_out.data_ptr()
+    st = lib().tl_rope_append(cache._ref, batch._ref, rope._ref,
+                              None if positions is None else _int32(positions, "positions", (batch.tokens,), device),
+                              qp, qs, heads, op, os_, kp, vp, elem, stride, _kv_raw_stream(stream, device))
+    if st:
+        _check(st, "tl_rope_append")
+
+
+def tree_positions(parents: torch.Tensor, token_offsets: torch.Tensor, start: torch.Tensor, positions: torch.Tensor, stream=None):
+    """positions (int32 [tokens]) = start of the row's request + the row's depth in its tree."""
+    _cuda(positions, "positions", torch.int32, 1)
+    device, n = positions.get_device(), positions.shape[0]
+    requests = start.shape[0]
+    _check(lib().tl_tree_positions(_int32(parents, "parents", (n,), device), _int32(token_offsets, "token_offsets", (requests + 1,), device),
+                                   _int32(start, "start", (requests,), device), requests, n, _int32(positions, "positions", (n,), device),
+                                   _kv_raw_stream(stream, device)), "tl_tree_positions")
+
+
+# ------------------------------------------------------------------ pages
+
+class PageTables(ctypes.Structure):
+    """tl_page_tables; keeps the tensors it was made from alive."""
+    _fields_ = [("page_table", _vp), ("held", _vp), ("holders", _vp), ("table_stride", _i64), ("requests", ctypes.c_int32),
+                ("pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32)]
+
+
+def page_tables(page_table: torch.Tensor, held: torch.Tensor, holders: torch.Tensor, page_tokens: int) -> PageTables:
+    """page_table: int32 [requests, n]; held: int32 [requests], pages of each; holders: int32 [pages], entries that name each page
+    (zeros for a pool that nobody uses yet, with held zeros)."""
+    _cuda(page_table, "page_table", torch.int32, 2), _cuda(holders, "holders", torch.int32, 1)
+    t = PageTables()
+    t._device = device = page_table.get_device()
+    t.requests, t.table_stride = page_table.shape
+    t.pages, t.page_tokens = holders.shape[0], int(page_tokens)
+    t.page_table = _int32(page_table, "page_table", page_table.shape, device)
+    t.held = _int32(held, "held", (t.requests,), device)
+    t.holders = _int32(holders, "holders", holders.shape, device)
+    t._tensors, t._ref = (page_table, held, holders), ctypes.byref(t)
+    return t
+
+
+def page_reserve(tables: PageTables, start: torch.Tensor, tokens: torch.Tensor, moves: torch.Tensor, n_moves: torch.Tensor,
+                 missing: torch.Tensor, stream=None):
+    """Pages for tokens[b] positions of every request (tokens[b] < 0: left alone), those of start[b] .. tokens[b] - 1 its own.  moves
+    (int32 [requests or more, 3]) and n_moves (int32 [1]): what page_copy is to do; missing (int32 [1]): free pages that lack (then
+    nothing has changed)."""
+    n, device = tables.requests, tables._device
+    if moves.shape[0] < n:
+        raise ValueError(f"moves: expected at least {n} rows")
+    st = lib().tl_page_reserve(tables._ref, _int32(start, "start", (n,), device), _int32(tokens, "tokens", (n,), device),
+                               _int32(moves, "moves", (moves.shape[0], 3), device), _int32(n_moves, "n_moves", (1,), device),
+                               _int32(missing, "missing", (1,), device), _kv_raw_stream(stream, device))
+    if st:
+        _check(st, "tl_page_reserve")
+
+
+def page_release(tables: PageTables, tokens: torch.Tensor | None = None, stream=None):
+    """Request b keeps the pages of its first tokens[b] positions (all if negative; tokens None: no request keeps any)."""
+    device = tables._device
+    st = lib().tl_page_release(tables._ref, None if tokens is None else _int32(tokens, "tokens", (tables.requests,), device),
+                               _kv_raw_stream(stream, device))
+    if st:
+        _check(st, "tl_page_release")
+
+
+def page_fork(tables: PageTables, from_: torch.Tensor, to: torch.Tensor, tokens: torch.Tensor, stream=None):
+    """Request to[f] (which holds nothing) shares the pages of the first tokens[f] positions of from_[f]."""
+    device, shape = tables._device, from_.shape
+    if len(shape) != 1:
+        raise ValueError("from_: expected [forks]")
+    st = lib().tl_page_fork(tables._ref, _int32(from_, "from_", shape, device), _int32(to, "to", shape, device),
+                            _int32(tokens, "tokens", shape, device), shape[0], _kv_raw_stream(stream, device))
+    if st:
+        _check(st, "tl_page_fork")
+
+
+def page_compact(tables: PageTables, moves: torch.Tensor, n_moves: torch.Tensor, in_use: torch.Tensor, stream=None):
+    """The pages in use move to the front of the pool, at most as many as moves (int32 [n, 3]) has rows; n_moves and in_use: int32 [1]."""
+    device = tables._device
+    if len(moves.shape) != 2:
+        raise ValueError("moves: expected [n, 3]")
+    st = lib().tl_page_compact(tables._ref, _int32(moves, "moves", (moves.shape[0], 3), device), moves.shape[0],
+                               _int32(n_moves, "n_moves", (1,), device), _int32(in_use, "in_use", (1,), device), _kv_raw_stream(stream, device))
+    if st:
+        _check(st, "tl_page_compact")
+
+
+def page_workspace_bytes(tables: PageTables, forks: int = 0) -> int:
+    return int(lib().tl_page_workspace_bytes(tables._ref, forks))
+
+
+def page_copy(cache: KvCache, moves: torch.Tensor, n_moves: torch.Tensor | None = None, to: KvCache | None = None, stream=None):
+    """For the first n_moves (all) rows of moves (int32 [n, 3]: from, to, tokens): copies the first tokens of a page of cache to a
+    page of `to` (the same cache by default)."""
+    device, dst = cache._device, cache if to is None else to
+    if dst._device != device:
+        raise ValueError(f"the caches lie on cuda:{device} and cuda:{dst._device}")
+    if len(moves.shape) != 2:
+        raise ValueError("moves: expected [n, 3]")
+    st = lib().tl_page_copy(cache._ref, dst._ref, _int32(moves, "moves", (moves.shape[0], 3), device),
+                            None if n_moves is None else _int32(n_moves, "n_moves", (1,), device), moves.shape[0],
+                            _kv_raw_stream(stream, device))
+    if st:
+        _check(st, "tl_page_copy")

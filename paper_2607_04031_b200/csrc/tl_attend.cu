@@ -87,15 +87,17 @@ __global__ void __launch_bounds__(kCombineThreads) attend_combine_kernel(const A
 int attend_small_bf16(bool, int, int, int*, int*, const AttendParams*, int, cudaStream_t);
 int attend_small_e4m3(bool, int, int, int*, int*, const AttendParams*, int, cudaStream_t);
 int attend_small_int8(bool, int, int, int*, int*, const AttendParams*, int, cudaStream_t);
+int attend_small_e2m1(bool, int, int, int*, int*, const AttendParams*, int, cudaStream_t);
 static auto attend_small_of(int format) {
-    return format == TL_KV_BF16 ? attend_small_bf16 : format == TL_KV_E4M3 ? attend_small_e4m3 : attend_small_int8;
+    return format == TL_KV_BF16 ? attend_small_bf16 : format == TL_KV_E4M3 ? attend_small_e4m3 : format == TL_KV_INT8 ? attend_small_int8 : attend_small_e2m1;
 }
 
 int attend_tc_bf16(int, int, const tl_kv_cache*, const AttendParams&, cudaStream_t);
 int attend_tc_e4m3(int, int, const tl_kv_cache*, const AttendParams&, cudaStream_t);
 int attend_tc_int8(int, int, const tl_kv_cache*, const AttendParams&, cudaStream_t);
+int attend_tc_e2m1(int, int, const tl_kv_cache*, const AttendParams&, cudaStream_t);
 static auto attend_tc_of(int format) {
-    return format == TL_KV_BF16 ? attend_tc_bf16 : format == TL_KV_E4M3 ? attend_tc_e4m3 : attend_tc_int8;
+    return format == TL_KV_BF16 ? attend_tc_bf16 : format == TL_KV_E4M3 ? attend_tc_e4m3 : format == TL_KV_INT8 ? attend_tc_int8 : attend_tc_e2m1;
 }
 
 // Which kernel a call runs, from what the host knows: the query rows per key/value head of an average request, and the

@@ -67,7 +67,8 @@ struct TcShape {
     static constexpr int kOffScale = kOffV + kVStages * kOperand;  // [stage][ks, log2 vs, 1 / vs][128]
     static constexpr int kOffStat = kOffScale + kVStages * 3 * kTcTile * 4;
     static constexpr int kOffBar = kOffStat + (kBlocks == 1 ? 2 * kTcTile * 16 : 0);
-    // 8-bit caches: codes on their way to conversion, 16 bytes per producer thread and round, one round kept in registers
+    // 8-bit caches: codes on their way to conversion, 16 bytes per producer thread and round, one round kept in registers (4-bit
+    // ones have half the rounds, and room for all of them)
     static constexpr int kRounds = kDim / 32;                      // of 256 threads x 16 bytes, per tile of keys or values
     static constexpr int kOffRaw = kOffBar + 256;
     static constexpr int kRawSlots = 2 * kRounds - 1;
@@ -176,7 +177,7 @@ static_assert(sizeof(TcBars) <= 256, "barrier block");
 template <int kDim, int kFmt, int kBlocks>
 __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_constant__ AttendTcParams tp) {
     using S = TcShape<kDim, kBlocks>;
-    constexpr bool kBf16 = kFmt == TL_KV_BF16;
+    constexpr bool kBf16 = kFmt == TL_KV_BF16, kFour = kFmt == TL_KV_E2M1;
     constexpr float kHead = attend_head(kFmt);
     extern __shared__ char smem_raw[];
     char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -333,7 +334,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     ++s_count;
                     tc_fence_after_sync();
                     const uint32_t meta = bars.meta[at];
-                    if (kFmt != TL_KV_INT8) odd |= *reinterpret_cast<const uint64_t*>(bars.odd[at]) != 0;
+                    if (kBf16 || kFmt == TL_KV_E4M3) odd |= *reinterpret_cast<const uint64_t*>(bars.odd[at]) != 0;
                     const int pos0 = (t0 + n) * kTcTile;
                     const bool edge = pos0 + kTcTile > w.a.r.start || meta != 0;
                     const float* const ks = scales + at * 3 * kTcTile + 2 * t4;
@@ -634,34 +635,45 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     return (__ballot_sync(0xffffffffu, bad) >> ((n & 3) * 8)) & 255u;
                 };
                 if (!kBf16) {
-                    constexpr int kPieces = kDim / 16;                       // 16-byte pieces of a row of codes
+                    constexpr int kPieces = kFour ? kDim / 32 : kDim / 16;   // 16-byte pieces of a row of codes
                     constexpr int kRowsPer = kTcProducerThreads / kPieces;   // rows one round of the threads covers
-                    constexpr int kRounds = S::kRounds;
+                    constexpr int kRounds = kFour ? S::kRounds / 2 : S::kRounds;
                     static_assert(kRounds * kRowsPer == kTcTile, "rounds");
+                    static_assert(2 * kRounds - (kFour ? 0 : 1) <= S::kRawSlots, "slots");
                     char* const raw_gen = smem + S::kOffRaw + pt * 16;
                     const uint32_t raw_mem = smem_u32(raw_gen);
                     // Eight neighbouring lanes cover four pieces of two rows: their stores of the swizzled halves fall on
                     // different banks (the two 64-dimension atoms of a row lie on the same ones).
-                    const int piece = kPieces == 8 ? (lane & 3) | (lane >> 4) << 2 : lane & 3;
-                    const int row0 = kPieces == 8 ? (pt >> 5) * 4 + ((lane >> 2) & 3) : pt >> 2;
+                    // (A piece of 4-bit codes is half of an atom's row: eight lanes cover the two of four rows.)
+                    const int piece = kFour ? (lane & 1) | (kPieces == 4 ? (lane >> 3 & 1) << 1 : 0) : kPieces == 8 ? (lane & 3) | (lane >> 4) << 2 : lane & 3;
+                    const int row0 = kFour ? (kPieces == 4 ? (pt >> 5) * 8 + (lane >> 1 & 3) + (lane >> 4) * 4 : pt >> 1)
+                                           : kPieces == 8 ? (pt >> 5) * 4 + ((lane >> 2) & 3) : pt >> 2;
                     const uint32_t within = uint32_t(row0 & 15) * uint32_t(p.cache.token_stride) + uint32_t(piece) * 16u;
                     const int scale_row = pt & 127, scale_of = pt >> 7;      // half of the threads fetch keys' scales, half values'
                     uint4 last = make_uint4(0, 0, 0, 0);                     // the values' last round
                     float sc = 0.0f;
                     bool sc_lack = false;
                     bool lack = false;                                       // its row does not exist
+                    uint32_t grp[2][kRounds];                                // 4-bit caches: the two group scales of a piece
                     // (Whole warp; the tile that `pages` has been turned to.)  Codes wait in shared memory, in slots that only this
                     // thread uses (a load's destination there takes no line of the first-level cache, which is small beside
                     // this kernel's shared memory); the last round, for which there is no slot, waits in registers.  Positions
                     // without a row are filled with zeros.
                     int64_t from[kRounds];                                   // of tile n + 1: byte offset in the pool, -1 without a row
+                    int64_t grp_from[kRounds];
                     auto locate = [&](int n) {
                         const int pos0 = (t0 + n) * kTcTile;
 #pragma unroll
                         for (int i = 0; i < kRounds; ++i) {
                             const int row = row0 + i * kRowsPer;
                             const int64_t at = place_of(n, row >> 4);
-                            from[i] = at >= 0 && pos0 + row < len ? at + within : -1;
+                            const bool in = at >= 0 && pos0 + row < len;
+                            from[i] = in ? at + within : -1;
+                            if (kFour) {
+                                const int page = page_of(n, row >> 4);
+                                grp_from[i] = (in ? int64_t(page) * p.cache.group_page_stride + ((pos0 + row) & pos_mask) * (kDim / 16) : 0) +
+                                              int64_t(w.head) * p.cache.group_head_stride + piece * 2;
+                            }
                         }
                     };
                     auto fetch = [&](int which) {
@@ -669,7 +681,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                         for (int i = 0; i < kRounds; ++i) {
                             const bool in = from[i] >= 0;
                             const char* const src = head_base[which] + (in ? from[i] : 0);
-                            if (which * kRounds + i < S::kRawSlots) {
+                            if (kFour) grp[which][i] = __ldg(reinterpret_cast<const uint16_t*>(p.cache.group[which] + grp_from[i]));
+                            if (kFour || which * kRounds + i < S::kRawSlots) {
                                 cp_async_16(raw_mem + uint32_t(which * kRounds + i) * 4096u, src, in);
                             } else {
                                 last = __ldg(reinterpret_cast<const uint4*>(src));
@@ -701,6 +714,23 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                         return odd;
                     };
                     auto store = [&](int which, char* base) {
+                        if constexpr (kFour) {
+                            const int c = (piece & 1) * 4;
+                            char* const to = base + (piece >> 1) * S::kAtomBytes + row0 * 128;
+#pragma unroll
+                            for (int i = 0; i < kRounds; ++i) {
+                                const uint4 raw = *reinterpret_cast<const uint4*>(raw_gen + (which * kRounds + i) * 4096);
+                                const uint32_t w4[4] = {raw.x, raw.y, raw.z, raw.w};
+                                const uint32_t g2[2] = {group_f16x2(grp[which][i], 0, 0, 0), group_f16x2(grp[which][i], 0, 1, 1)};
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) {
+                                    uint32_t h[4];
+                                    e2m1x8_to_f16(w4[k], g2[k >> 1], h);
+                                    *reinterpret_cast<uint4*>(to + i * kRowsPer * 128 + (((c + k) ^ (row0 & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                                }
+                            }
+                            return;
+                        }
                         const int c = (piece & 3) * 2;
                         char* const at0 = base + (piece >> 2) * S::kAtomBytes + row0 * 128 + ((c ^ (row0 & 7)) << 4);
                         char* const at1 = base + (piece >> 2) * S::kAtomBytes + row0 * 128 + (((c + 1) ^ (row0 & 7)) << 4);
@@ -750,7 +780,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                             const bool odd = kFmt == TL_KV_E4M3 && own_from < kTcTile && take_nan_out(own_from);
                             store(1, smem + S::kOffV + vi * S::kOperand);
                             float* const to = scales + vi * 3 * kTcTile + scale_row;
-                            const float s_now = sc_lack ? 0.0f : sc;
+                            const float s_now = sc_lack ? 0.0f : kFour ? sc * kGroupUnit : sc;
                             if (scale_of == 0) {
                                 to[0] = s_now;
                             } else {

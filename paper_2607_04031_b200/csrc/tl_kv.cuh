@@ -11,7 +11,8 @@ namespace tl {
 
 enum : uint32_t {
     kBadPage = 0xA00,           // a page-table entry outside the cache, or a position past the table's last page
-    kBadAccepted = 0xB00        // tl_kv_commit: an accepted index outside the request's tokens
+    kBadAccepted = 0xB00,       // tl_kv_commit: an accepted index outside the request's tokens
+    kBadFork = 0xD00            // tl_page_fork: a request outside the tables, or one that is taken
 };
 
 // tl_kv_cache as the kernels use it: strides in bytes, page size as a shift.
@@ -20,6 +21,8 @@ struct KvView {
     float* scale[2];
     int64_t page_stride, head_stride, token_stride;     // bytes
     int64_t scale_page_stride, scale_head_stride;       // floats
+    char* group[2];             // 4-bit caches: a byte per 16 elements
+    int64_t group_page_stride, group_head_stride;       // bytes
     int64_t pages;
     int heads, page_shift;
 };
@@ -41,7 +44,10 @@ int kv_batch_view(const tl_kv_batch* b, KvBatchView* out);
 template <typename... P>
 inline bool words_aligned(const P*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 3u) == 0; }
 
-inline int kv_item(int format) { return format == TL_KV_BF16 ? 2 : 1; }
+// Bytes of `elements` elements.
+inline constexpr int64_t kv_bytes(int format, int64_t elements) {
+    return format == TL_KV_BF16 ? elements * 2 : format == TL_KV_E2M1 ? elements / 2 : elements;
+}
 
 #ifdef __CUDACC__
 
@@ -79,6 +85,28 @@ __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool 
 __device__ __forceinline__ void cp_async_8(uint32_t dst, const void* src, bool valid) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(valid ? 8 : 0) : "memory");
 }
+__device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src, bool valid) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(valid ? 4 : 0) : "memory");
+}
+template <int kBytes>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool valid) {
+    if (kBytes == 16) cp_async_16(dst, src, valid);
+    else if (kBytes == 8) cp_async_8(dst, src, valid);
+    else cp_async_4(dst, src, valid);
+}
+// 4, 8 or 16 bytes of shared memory.
+template <int kBytes>
+__device__ __forceinline__ void load_words(const char* src, uint32_t (&w)[4]) {
+    if (kBytes == 16) {
+        const uint4 x = *reinterpret_cast<const uint4*>(src);
+        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+    } else if (kBytes == 8) {
+        const uint2 x = *reinterpret_cast<const uint2*>(src);
+        w[0] = x.x, w[1] = x.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(src);
+    }
+}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kPending>
 __device__ __forceinline__ void cp_async_wait() {
@@ -103,6 +131,34 @@ __device__ __forceinline__ uint32_t s8x2_from_biased(uint32_t pair_with_64) {
     uint32_t r;
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(pair_with_64), "r"(0x64806480u));
     return r;
+}
+// Two E2M1 codes (byte kByte of x) to two f16 values.
+template <int kByte>
+__device__ __forceinline__ uint32_t e2m1x2_to_f16x2(uint32_t x) {
+    uint32_t r;
+    if (kByte == 0) asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\t}" : "=r"(r) : "r"(x));
+    if (kByte == 1) asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b;\n\t}" : "=r"(r) : "r"(x));
+    if (kByte == 2) asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, c;\n\t}" : "=r"(r) : "r"(x));
+    if (kByte == 3) asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, d;\n\t}" : "=r"(r) : "r"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t f16x2_mul(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// Group scales to f16, times 2^-8: an E4M3 byte's exponent and mantissa moved into an f16's read 2^-8 of the value (0x7f: 480 of it),
+// and code times that is exact: 6 bits, a multiple of 2^-18, at most 11.25.  lo and hi: the halves' bytes, 0 .. 3 of a, 4 .. 7 of b.
+constexpr float kGroupUnit = 256.0f;
+__device__ __forceinline__ uint32_t group_f16x2(uint32_t a, uint32_t b, int lo, int hi) {
+    return (__byte_perm(a, b, uint32_t(lo << 4 | hi << 12)) >> 1) & 0x3f803f80u;
+}
+// Eight codes of a word, times their group scale (f16x2_mul's second operand): four f16x2 registers.
+__device__ __forceinline__ void e2m1x8_to_f16(uint32_t w, uint32_t scale, uint32_t (&h)[4]) {
+    h[0] = f16x2_mul(e2m1x2_to_f16x2<0>(w), scale);
+    h[1] = f16x2_mul(e2m1x2_to_f16x2<1>(w), scale);
+    h[2] = f16x2_mul(e2m1x2_to_f16x2<2>(w), scale);
+    h[3] = f16x2_mul(e2m1x2_to_f16x2<3>(w), scale);
 }
 // Four codes of one 32-bit word to two f16x2 registers.
 template <int kFmt>
