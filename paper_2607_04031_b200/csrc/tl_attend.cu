@@ -130,7 +130,8 @@ static int attend_plan(const tl_kv_cache* cache, const tl_kv_batch* batch, int q
         const double tiles256 = cache->heads * double(ceil_div(rows, 256)) * std::ceil(positions / 128);
         plan->mma_rows = rows >= kBlockRowsFrom && tiles256 >= double(kBlockTilesFrom * sms) ? 256 : 128;
     } else {
-        plan->mma_rows = rows > 16 && cache->head_dim <= 128 ? 32 : 16;
+        // (the kernel for 4-bit caches takes rows by eights)
+        plan->mma_rows = cache->format == TL_KV_E2M1 && rows <= 8 ? 8 : rows > 16 && cache->head_dim <= 128 ? 32 : 16;
         if (int rc = attend_small_of(cache->format)(false, cache->head_dim, plan->mma_rows, &plan->tile_tokens, &plan->ctas_per_sm, nullptr, 0, nullptr)) return rc;
     }
     // no more CTAs than there can be tiles (the length is bounded by the page table)
@@ -214,7 +215,7 @@ int tl_tree_attention(const tl_kv_cache* cache, const tl_kv_batch* batch, const 
         return rc;
     if (plan.part_bytes == 0) return TL_OK;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(plan.ctas - 1), unsigned(plan.mma_rows / kCombineRows));
+    cfg.gridDim = dim3(unsigned(plan.ctas - 1), unsigned(std::max(plan.mma_rows / kCombineRows, 1)));
     cfg.blockDim = dim3(kCombineThreads);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];

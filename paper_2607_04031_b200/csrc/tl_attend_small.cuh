@@ -10,8 +10,8 @@
 // q k^T, tokens 2t, 2t+1, 2t+8, 2t+9 for p v) with cp.async into slots that only it reads, several tiles ahead, and
 // its registers are the instruction's B fragments after the conversion:
 //   q k^T: 4 consecutive codes of a token are the fragment of one 16-deep step;
-//   p v:   codes of two tokens at the same dimensions, interleaved bytewise (4-bit codes: by half bytes), are one fragment pair each.
-// 8-bit codes become f16 (exact for both formats), and so do 4-bit codes times their group scale; q becomes f16 scaled by a power of two per row (exact but for
+//   p v:   codes of two tokens at the same dimensions, interleaved bytewise, are one fragment pair each.
+// 8-bit codes become f16 (exact for both formats), q becomes f16 scaled by a power of two per row (exact but for
 // elements 2^-31 below the row's largest).  The key's scale multiplies the score.  The value's scale goes into the
 // exponent, w_j = 2^(s_j + log2 vs_j - m), with m following the maximum of s_j + log2 vs_j (attend_head): w is as exact as f16
 // can be where the contribution w_j v_j is large, and the softmax sum is that of w_j / vs_j.  The second product
@@ -33,26 +33,21 @@ struct SmallNo { static constexpr bool value = false; };
 template <int kDim, int kFmt, int kMT>
 struct SmallShape {
     static constexpr bool kBf16 = kFmt == TL_KV_BF16;
-    static constexpr bool kFour = kFmt == TL_KV_E2M1;
+    static constexpr int kItem = kBf16 ? 2 : 1;
     static constexpr float kHead = attend_head(kFmt);
-    static constexpr int kRowBytes = int(kv_bytes(kFmt, kDim));
-    static constexpr int kWide = kFour ? kDim : kRowBytes;         // (4 bits take the registers that 8 take)
-    static constexpr int kCtasPerSm = kMT == 1 && kWide == 128 ? 3 : kMT == 1 && kWide < 128 ? 2 : 1;
+    static constexpr int kRowBytes = kDim * kItem;
+    static constexpr int kCtasPerSm = kMT == 1 && kRowBytes == 128 ? 3 : kMT == 1 && kRowBytes < 128 ? 2 : 1;
     static constexpr int kWarps = kDim == 256 || kCtasPerSm == 3 ? 4 : 8;
     static constexpr int kThreads = kWarps * 32;
     static constexpr int kRows = kMT * 16;
     static constexpr int kTile = kWarps * 16;
     static constexpr int kSteps = kDim / 16;                       // 16-deep steps of q k^T
-    static constexpr int kKBytes = kRowBytes / 4 < 16 ? kRowBytes / 4 : 16;
-    static constexpr int kKChunks = kRowBytes / 4 / kKBytes;       // pieces of a token per thread (4 threads a row)
-    static constexpr int kKPiece = kKBytes * kDim / kRowBytes;  // elements of one
+    static constexpr int kKChunks = kRowBytes / 64;                // 16-byte pieces of a token per thread (4 threads a row)
     static constexpr int kVBytes = kRowBytes / 8 < 16 ? kRowBytes / 8 : 16;
     static constexpr int kVChunks = kRowBytes / 8 / kVBytes;       // pieces of a token per thread (8 threads a row)
-    static constexpr int kVPiece = kVBytes * kDim / kRowBytes;
     static constexpr int kNTiles = kDim / 8;                       // 8-wide column tiles of p v
-    static constexpr int kScaleAt = 32 * kRowBytes, kGroupAt = kScaleAt + 128, kGroups = kDim / 16;
-    static constexpr int kStageBytes = kGroupAt + (kFour ? 32 * kGroups : 0);   // one warp's 16 tokens, keys and values, and the scales
-    static constexpr int kSub = kMT == 1 && kWide <= 128 ? 2 : 1;  // sub-tiles a warp takes at a time
+    static constexpr int kStageBytes = 32 * kRowBytes + 128;       // one warp's 16 tokens, keys and values, and the scales
+    static constexpr int kSub = kMT == 1 && kRowBytes <= 128 ? 2 : 1;   // sub-tiles a warp takes at a time
     static constexpr int kQBytes = kMT * kSteps * 512;
     static constexpr int kStatBytes = (kWarps * kRows * 2 + kRows * 4) * 4;
     static constexpr int kLimit = (kCtasPerSm == 3 ? 74 : kCtasPerSm == 2 ? 112 : 225) * 1024;
@@ -114,7 +109,7 @@ attend_kernel(const AttendParams p) {
         uint32_t bad_any = 0;
         // (offsets within a sub-tile fit 32 bits: the host bounds the token stride)
         const uint32_t ts = uint32_t(p.cache.token_stride);
-        const uint32_t k_off = uint32_t(g) * ts + uint32_t(t) * uint32_t(S::kKBytes), v_off = uint32_t(2 * t) * ts + uint32_t(g) * uint32_t(S::kVBytes);
+        const uint32_t k_off = uint32_t(g) * ts + uint32_t(t) * 16u, v_off = uint32_t(2 * t) * ts + uint32_t(g) * uint32_t(S::kVBytes);
         auto issue = [&](int i) {                                        // starts the copies of sub-tile i (whole warp, i upwards)
             if (i < count) {
                 if (i > 0 && (i & 31) == 0) {
@@ -138,7 +133,7 @@ attend_kernel(const AttendParams p) {
                         const char* src = in ? k_at + (k_off + uint32_t(8 * h) * ts) : k_head;
 #pragma unroll
                         for (int c = 0; c < S::kKChunks; ++c)
-                            cp_async<S::kKBytes>(dst + uint32_t((h * S::kKChunks + c) * 32 * S::kKBytes + lane * S::kKBytes), src + c * 64, in);
+                            cp_async_16(dst + uint32_t((h * S::kKChunks + c) * 512 + lane * 16), src + c * 64, in);
                     }
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
@@ -148,7 +143,8 @@ attend_kernel(const AttendParams p) {
 #pragma unroll
                         for (int c = 0; c < S::kVChunks; ++c) {
                             const uint32_t to = dst + uint32_t(16 * S::kRowBytes + (k * S::kVChunks + c) * 32 * S::kVBytes + lane * S::kVBytes);
-                            cp_async<S::kVBytes>(to, src + c * 128, in);
+                            if (S::kVBytes == 16) cp_async_16(to, src + c * 128, in);
+                            else cp_async_8(to, src, in);
                         }
                     }
                 };
@@ -157,12 +153,7 @@ attend_kernel(const AttendParams p) {
                 if (!kBf16 && lane < 8) {
                     // (the scales of a page's 16 tokens are read whole; those past the end belong to masked positions)
                     const float* sc = p.cache.scale[lane >> 2] + (ok ? int64_t(page) * p.cache.scale_page_stride + int64_t(w.head) * p.cache.scale_head_stride + line : 0);
-                    cp_async_16(dst + uint32_t(S::kScaleAt + lane * 16), sc + (ok ? (lane & 3) * 4 : 0), ok);
-                }
-                if (S::kFour && lane < 2 * S::kGroups) {
-                    // (those of a page's 16 tokens are one run too)
-                    const char* gr = p.cache.group[lane / S::kGroups] + (ok ? int64_t(page) * p.cache.group_page_stride + int64_t(w.head) * p.cache.group_head_stride + line * S::kGroups : 0);
-                    cp_async_16(dst + uint32_t(S::kGroupAt + lane * 16), gr + (ok ? lane % S::kGroups * 16 : 0), ok);
+                    cp_async_16(dst + uint32_t(32 * S::kRowBytes + lane * 16), sc + (ok ? (lane & 3) * 4 : 0), ok);
                 }
             }
             cp_async_commit();
@@ -202,12 +193,12 @@ attend_kernel(const AttendParams p) {
                 mul = __uint_as_float(uint32_t(127 + up) << 23);
                 fac *= __uint_as_float(uint32_t(127 - up) << 23);
             }
-            if (lane == 0) row_fac[r] = S::kFour ? fac * kGroupUnit : fac;
+            if (lane == 0) row_fac[r] = fac;
             __half* const frag16 = reinterpret_cast<__half*>(q_frag);
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const int d = lane * kPer + i;
-                constexpr int kPiece = S::kKPiece;
+                constexpr int kPiece = kBf16 ? 8 : 16;                 // elements of a 16-byte piece of the cache row
                 const int c = d / (4 * kPiece), tt = d / kPiece % 4, ii = d % kPiece;
                 const int step = c * (kPiece / 4) + ii / 4, reg = (r % 16 >= 8 ? 1 : 0) + 2 * (ii % 4 / 2);
                 const int at = (((r / 16) * S::kSteps + step) * 32 + (r % 8) * 4 + tt) * 8 + reg * 2 + (ii & 1);
@@ -258,21 +249,14 @@ attend_kernel(const AttendParams p) {
             }
 #pragma unroll
             for (int c = 0; c < S::kKChunks; ++c) {
-                constexpr int kStepsPer = S::kKPiece / 4;
+                constexpr int kStepsPer = kBf16 ? 2 : 4;
                 uint32_t a0[S::kSub][4], a1[S::kSub][4];
-                uint32_t g0[S::kSub][2], g1[S::kSub][2];               // 4-bit caches: group scales of the two tokens' pieces
-                uint32_t b4[S::kSub][2][4];                            // and eight of their codes, converted
 #pragma unroll
                 for (int u = 0; u < S::kSub; ++u) {
-                    load_words<S::kKBytes>(st[u] + c * 32 * S::kKBytes + lane * S::kKBytes, a0[u]);
-                    load_words<S::kKBytes>(st[u] + (S::kKChunks + c) * 32 * S::kKBytes + lane * S::kKBytes, a1[u]);
-                    if (S::kFour) {
-                        const char* const gr = st[u] + S::kGroupAt + g * S::kGroups + (c * 4 + t) * (S::kKPiece / 16);
-                        const uint32_t x0 = S::kKPiece == 32 ? *reinterpret_cast<const uint16_t*>(gr) : uint8_t(*gr);
-                        const uint32_t x1 = S::kKPiece == 32 ? *reinterpret_cast<const uint16_t*>(gr + 8 * S::kGroups) : uint8_t(gr[8 * S::kGroups]);
-                        g0[u][0] = group_f16x2(x0, 0, 0, 0), g0[u][1] = group_f16x2(x0, 0, 1, 1);
-                        g1[u][0] = group_f16x2(x1, 0, 0, 0), g1[u][1] = group_f16x2(x1, 0, 1, 1);
-                    }
+                    const uint4 k0 = *reinterpret_cast<const uint4*>(st[u] + c * 512 + lane * 16);
+                    const uint4 k1 = *reinterpret_cast<const uint4*>(st[u] + (S::kKChunks + c) * 512 + lane * 16);
+                    a0[u][0] = k0.x, a0[u][1] = k0.y, a0[u][2] = k0.z, a0[u][3] = k0.w;
+                    a1[u][0] = k1.x, a1[u][1] = k1.y, a1[u][2] = k1.z, a1[u][3] = k1.w;
                 }
 #pragma unroll
                 for (int q = 0; q < kStepsPer; ++q) {
@@ -285,16 +269,9 @@ attend_kernel(const AttendParams p) {
 #pragma unroll
                     for (int u = 0; u < S::kSub; ++u) {
                         uint32_t b00, b01, b10, b11;
-                        if constexpr (kBf16) {
+                        if (kBf16) {
                             b00 = a0[u][(2 * q) & 3], b01 = a0[u][(2 * q + 1) & 3];
                             b10 = a1[u][(2 * q) & 3], b11 = a1[u][(2 * q + 1) & 3];
-                        } else if constexpr (S::kFour) {
-                            if (q % 2 == 0) {
-                                e2m1x8_to_f16(a0[u][(q / 2) & 3], g0[u][(q / 4) & 1], b4[u][0]);
-                                e2m1x8_to_f16(a1[u][(q / 2) & 3], g1[u][(q / 4) & 1], b4[u][1]);
-                            }
-                            b00 = b4[u][0][q % 2 * 2], b01 = b4[u][0][q % 2 * 2 + 1];
-                            b10 = b4[u][1][q % 2 * 2], b11 = b4[u][1][q % 2 * 2 + 1];
                         } else {
                             codes4_to_f16<kFmt>(a0[u][q & 3], b00, b01);
                             codes4_to_f16<kFmt>(a1[u][q & 3], b10, b11);
@@ -314,12 +291,11 @@ attend_kernel(const AttendParams p) {
 #pragma unroll
             for (int u = 0; u < S::kSub; ++u) {
                 if (!kBf16) {
-                    const float* sc = reinterpret_cast<const float*>(st[u] + S::kScaleAt);
+                    const float* sc = reinterpret_cast<const float*>(st[u] + 32 * S::kRowBytes);
 #pragma unroll
                     for (int nt = 0; nt < 2; ++nt) {
                         const float2 ks = *reinterpret_cast<const float2*>(sc + nt * 8 + 2 * t);
-                        float2 vs = *reinterpret_cast<const float2*>(sc + 16 + nt * 8 + 2 * t);
-                        if (S::kFour) vs.x *= kGroupUnit, vs.y *= kGroupUnit;
+                        const float2 vs = *reinterpret_cast<const float2*>(sc + 16 + nt * 8 + 2 * t);
                         // A row of zero values has scale 0: the floor in its place gives it its share of the sum.  A NaN
                         // scale reaches the score alone (the product with 0), which a mask can still replace.
                         const float v0 = vs.x >= kScaleFloor ? vs.x : kScaleFloor, v1 = vs.y >= kScaleFloor ? vs.y : kScaleFloor;
@@ -471,21 +447,17 @@ attend_kernel(const AttendParams p) {
 #pragma unroll
                 for (int c = 0; c < S::kVChunks; ++c) {
                     constexpr int kWords = S::kVBytes / 4;
-                    uint32_t v[4][4];
+                    uint32_t v[4][kWords];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) load_words<S::kVBytes>(vst + (k * S::kVChunks + c) * 32 * S::kVBytes + lane * S::kVBytes, v[k]);
-                    // 4-bit caches: group scales of the thread's pieces of tokens 2t, 2t + 1 and of 2t + 8, 2t + 9, side by side
-                    uint32_t g01[2], g89[2];
-                    if (S::kFour) {
-                        const char* const gr = st[u] + S::kGroupAt + (16 + 2 * t) * S::kGroups + g * S::kVPiece / 16;
-                        uint32_t x[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const char* const at = gr + ((k & 1) + 8 * (k >> 1)) * S::kGroups;
-                            x[k] = S::kVPiece == 32 ? *reinterpret_cast<const uint16_t*>(at) : uint8_t(*at);
+                    for (int k = 0; k < 4; ++k) {
+                        const char* src = vst + (k * S::kVChunks + c) * 32 * S::kVBytes + lane * S::kVBytes;
+                        if (S::kVBytes == 16) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(src);
+                            v[k][0] = x.x, v[k][1 % kWords] = x.y, v[k][2 % kWords] = x.z, v[k][3 % kWords] = x.w;
+                        } else {
+                            const uint2 x = *reinterpret_cast<const uint2*>(src);
+                            v[k][0] = x.x, v[k][1 % kWords] = x.y;
                         }
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) g01[i] = group_f16x2(x[0], x[1], i, 4 + i), g89[i] = group_f16x2(x[2], x[3], i, 4 + i);
                     }
                     if (kFmt == TL_KV_E4M3 && edge[u]) {
                         // Among the step's own tokens, of which rows see different ones: a NaN code stays out of the product (a weight
@@ -505,7 +477,7 @@ attend_kernel(const AttendParams p) {
                     }
 #pragma unroll
                     for (int q = 0; q < kWords; ++q) {
-                        if constexpr (kBf16) {
+                        if (kBf16) {
                             const uint32_t b[4] = {__byte_perm(v[0][q], v[1][q], 0x5410), __byte_perm(v[2][q], v[3][q], 0x5410),
                                                    __byte_perm(v[0][q], v[1][q], 0x7632), __byte_perm(v[2][q], v[3][q], 0x7632)};
 #pragma unroll
@@ -515,20 +487,6 @@ attend_kernel(const AttendParams p) {
                                 mma_16816<true>(o[mt][(c * kWords + q) * 2], a_low[mt], b[0], b[1]);
                                 mma_16816<true>(o[mt][(c * kWords + q) * 2 + 1], a_low[mt], b[2], b[3]);
                             }
-                        } else if constexpr (S::kFour) {
-                            // the two tokens' codes of one dimension become the halves of a byte
-                            constexpr uint32_t kLow = 0x0f0f0f0fu;
-                            uint32_t lo[2][4], hi[2][4];
-                            const int i = q / 2 & 1;
-                            e2m1x8_to_f16((v[0][q] & kLow) | (v[1][q] << 4 & ~kLow), g01[i], lo[0]);
-                            e2m1x8_to_f16((v[0][q] >> 4 & kLow) | (v[1][q] & ~kLow), g01[i], lo[1]);
-                            e2m1x8_to_f16((v[2][q] & kLow) | (v[3][q] << 4 & ~kLow), g89[i], hi[0]);
-                            e2m1x8_to_f16((v[2][q] >> 4 & kLow) | (v[3][q] & ~kLow), g89[i], hi[1]);
-#pragma unroll
-                            for (int z = 0; z < 8; ++z)
-#pragma unroll
-                                for (int mt = 0; mt < kMT; ++mt)
-                                    mma_16816<false>(o[mt][(c * kWords + q) * 8 + z], a[mt], lo[z & 1][z >> 1], hi[z & 1][z >> 1]);
                         } else {
                             uint32_t lo[4], hi[4];
                             codes4_to_f16<kFmt>(__byte_perm(v[0][q], v[1][q], 0x5140), lo[0], lo[1]);
@@ -586,7 +544,7 @@ attend_kernel(const AttendParams p) {
 #pragma unroll
                     for (int j = 0; j < S::kNTiles; j += 4) {
                         // columns of tile j .. j + 3 are consecutive dimensions within this thread's piece
-                        constexpr int kPiece = S::kVPiece;
+                        constexpr int kPiece = kBf16 ? 8 : S::kVBytes;
                         const int d = (j / kPiece) * 8 * kPiece + (2 * t + e) * kPiece + j % kPiece;
                         *reinterpret_cast<float4*>(dst + d) = make_float4(o[mt][j][2 * h + e] * f, o[mt][j + 1][2 * h + e] * f,
                                                                           o[mt][j + 2][2 * h + e] * f, o[mt][j + 3][2 * h + e] * f);

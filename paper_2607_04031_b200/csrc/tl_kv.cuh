@@ -85,15 +85,6 @@ __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool 
 __device__ __forceinline__ void cp_async_8(uint32_t dst, const void* src, bool valid) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(valid ? 8 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src, bool valid) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(valid ? 4 : 0) : "memory");
-}
-template <int kBytes>
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool valid) {
-    if (kBytes == 16) cp_async_16(dst, src, valid);
-    else if (kBytes == 8) cp_async_8(dst, src, valid);
-    else cp_async_4(dst, src, valid);
-}
 // 4, 8 or 16 bytes of shared memory.
 template <int kBytes>
 __device__ __forceinline__ void load_words(const char* src, uint32_t (&w)[4]) {
