@@ -2,9 +2,9 @@
 //
 // The bookkeeping calls are integer work on tables that live on the device, so what they decide must not depend on the order in which
 // threads arrive: fresh pages are the lowest free ones in the order of requests and entries, ranks come from prefix sums, and the
-// atomics used (counts and minima of integers) give the same result in any order.  reserve, fork and compact run as one cluster of
-// kCtas CTAs, each with a share of the pool and of the requests; what the CTAs tell one another goes through the workspace, between
-// barriers of the cluster.
+// atomics used (counts and minima of integers) give the same result in any order.  reserve and compact look through the whole pool,
+// 32 pages per thread, in one CTA or (a large pool) one cluster; what threads tell one another goes through the workspace, between
+// barriers.
 #include "tl_kv_rows.cuh"
 
 #include <algorithm>
@@ -19,7 +19,10 @@ struct PageView {
     int requests, pages, page_shift;
 };
 
-constexpr int kPageCtas = 8, kPageThreads = 1024, kPageWarps = kPageThreads / 32;
+constexpr int kPageThreads = 1024, kPageWarps = kPageThreads / 32;
+// CTAs that look through a pool: one, whose barriers cost next to nothing, up to 2^17 pages, else a cluster of eight (the barrier of a
+// cluster that orders global memory took about a microsecond, and there are five of them).
+constexpr int kPageCtas = 8, kPagesOfOne = 1 << 17;
 
 // What a reserving call keeps per page it may take from somebody (written before it is read).
 struct PageClaim {
@@ -28,10 +31,12 @@ struct PageClaim {
     uint32_t pad;
 };
 
-// Orders everything the cluster's threads have done before, global memory included.
+// Orders everything the threads have done before, global memory included.
+template <int kCtas>
 __device__ __forceinline__ void page_sync() {
     __syncwarp();                                             // (loops in front of it may end lane by lane)
-    cluster_sync();
+    if (kCtas > 1) cluster_sync();
+    else __syncthreads();
 }
 
 // Sum of one number per thread in front of the thread, and of all (whole CTA).
@@ -59,11 +64,33 @@ __device__ __forceinline__ T block_scan(T x, T* shared, T* total) {
 }
 static_assert(kPageWarps == 32, "block_scan");
 
-// The CTA's share of the pool: a multiple of four pages, in order.
-__device__ __forceinline__ void pool_share(int pages, int rank, int* from, int* to) {
-    const int64_t each = ((int64_t(pages) + kPageCtas - 1) / kPageCtas + 3) / 4 * 4;
-    *from = int(min(int64_t(pages), rank * each));
-    *to = int(min(int64_t(pages), (rank + 1) * each));
+// The pool is looked through 32 pages per thread at a time, in the order of turns, CTAs and threads.  Bit i: page first + i is free
+// (or, used: is in use); pages past the end are neither.  Whole warp (of consecutive threads): a load of 32 neighbouring pages gives
+// one thread its word.
+__device__ __forceinline__ uint32_t page_bits(const PageView& t, int64_t first, bool used) {
+    const int lane = int(lane_id());
+    const int64_t base = first - int64_t(lane) * 32;
+    uint32_t bits = 0;
+    int v[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        const int64_t i = base + j * 32 + lane;
+        v[j] = i < t.pages ? t.holders[i] : used ? 0 : 1;
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        const uint32_t word = __ballot_sync(0xffffffffu, (v[j] == 0) != used);
+        if (lane == j) bits = word;
+    }
+    return bits;
+}
+// Sum of the first n numbers of a list, by a whole warp.
+__device__ __forceinline__ int64_t warp_sum(const int32_t* list, int n) {
+    int64_t sum = 0;
+    for (int i = int(lane_id()); i < n; i += 32) sum += list[i];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    return sum;
 }
 
 struct ReserveParams {
@@ -74,163 +101,235 @@ struct ReserveParams {
     int32_t* n_moves;
     int32_t* missing;
     PageClaim* claims;                   // [pages]
-    int32_t* fresh;                      // [requests]: fresh pages it needs, then how many the requests in front of it need
-    int32_t* copies;                     // [requests]: likewise pages to copy
     int32_t* free_list;                  // [pages]: the pages to be taken, then those given up for them (-1: none)
-    int32_t* cta_free;                   // [kPageCtas]
+    int32_t* counts;                     // (cluster) [turns of the pool * CTAs]: free pages
+    int32_t* fresh;                      // (cluster) [turns of the requests * CTAs]: pages to be taken, one CTA's (at most INT32_MAX)
+    int32_t* copies;                     // (cluster) likewise pages to copy
     uint32_t* status;
 };
 
 struct ReserveRange {
     int have, need;                      // pages held and wanted
     int first, last;                     // entries to be written among those held
-    int start;
+    int line;                            // rows of entry `first` in front of the position it is written from
 };
 __device__ __forceinline__ ReserveRange reserve_range(const ReserveParams& p, int b, bool* clipped) {
-    ReserveRange r;
-    const int tokens = p.tokens[b];
-    r.start = max(p.start[b], 0);
+    ReserveRange r = {0, 0, 0, 0, 0};
+    if (b >= p.t.requests) return r;
+    const int tokens = p.tokens[b], start = max(p.start[b], 0);
     r.have = int(min(int64_t(max(p.t.held[b], 0)), p.t.table_stride));
     const int64_t need = tokens < 0 ? 0 : (int64_t(tokens) + (1 << p.t.page_shift) - 1) >> p.t.page_shift;
     if (need > p.t.table_stride) *clipped = true;
     r.need = int(min(need, p.t.table_stride));
-    r.first = r.start >> p.t.page_shift;
-    r.last = tokens > r.start ? min(r.need, r.have) : 0;
+    r.first = start >> p.t.page_shift;
+    r.last = tokens > start ? min(r.need, r.have) : 0;
+    r.line = start & ((1 << p.t.page_shift) - 1);
     return r;
 }
-// Whether an entry's page has other holders.
-__device__ __forceinline__ bool entry_shared(const PageView& t, int page) { return page >= 0 && page < t.pages && t.holders[page] > 1; }
-// Whether the entry gives its shared page up (another of those that are to write it keeps it, or somebody who is not).
-__device__ __forceinline__ bool entry_leaves(const ReserveParams& p, int b, int e, int page) {
-    const PageClaim c = p.claims[page];
-    return !(int64_t(c.here) == p.t.holders[page] && c.first == (static_cast<unsigned long long>(b) << 32 | uint32_t(e)));
+// Calls f(request, entry, page) for every entry to be written, a request per lane; f's result (0 or 1) is added up for the request.
+// Few entries are their lane's, a long range is taken by the whole warp.
+template <typename F>
+__device__ __forceinline__ int for_entries(const PageView& t, int b, const ReserveRange& r, F f) {
+    constexpr int kFew = 2;
+    const int n = max(r.last - r.first, 0);
+    int sum = 0;
+    if (n <= kFew)
+        for (int e = r.first; e < r.last; ++e) sum += f(b, e, t.table[int64_t(b) * t.table_stride + e]);
+    __syncwarp();
+    for (uint32_t many = __ballot_sync(0xffffffffu, n > kFew); many; many &= many - 1) {
+        const int l = __ffs(int(many)) - 1, b1 = __shfl_sync(0xffffffffu, b, l);
+        const int first = __shfl_sync(0xffffffffu, r.first, l), last = __shfl_sync(0xffffffffu, r.last, l);
+        int part = 0;
+        for (int e = first + int(lane_id()); e < last; e += 32) part += f(b1, e, t.table[int64_t(b1) * t.table_stride + e]);
+        part = __reduce_add_sync(0xffffffffu, part);
+        if (int(lane_id()) == l) sum = part;
+    }
+    return sum;
 }
 
-__global__ void __cluster_dims__(kPageCtas, 1, 1) __launch_bounds__(kPageThreads) page_reserve_kernel(const ReserveParams p) {
+template <int kCtas>
+__global__ void __launch_bounds__(kPageThreads) page_reserve_kernel(const ReserveParams p) {
     __shared__ int64_t sums_wide[kPageWarps];
     __shared__ int sums[kPageWarps];
     pdl_wait();
     pdl_launch_dependents();
-    const int rank = int(cluster_cta_rank()), lane = int(lane_id()), warp = rank * kPageWarps + int(threadIdx.x) / 32;
-    constexpr int kWarps = kPageCtas * kPageWarps;
+    const int rank = kCtas > 1 ? int(cluster_cta_rank()) : 0, lane = int(lane_id());
+    constexpr int kAll = kCtas * kPageThreads;
+    const int thread = rank * kPageThreads + int(threadIdx.x);
+    const int turns = int((int64_t(p.t.pages) + kAll * 32 - 1) / (kAll * 32)), rounds = (p.t.requests + kAll - 1) / kAll;
     bool clipped = false, bad = false;
-    // claims on shared pages: cleared, then counted
-    for (int b = warp; b < p.t.requests; b += kWarps) {
-        const ReserveRange r = reserve_range(p, b, &clipped);
-        for (int e = r.first + lane; e < r.last; e += 32) {
-            const int page = p.t.table[int64_t(b) * p.t.table_stride + e];
-            bad |= page < 0 || page >= p.t.pages;
-            if (entry_shared(p.t, page)) p.claims[page] = PageClaim{~0ull, 0u, 0u};
-        }
-    }
-    page_sync();
-    for (int b = warp; b < p.t.requests; b += kWarps) {
-        const ReserveRange r = reserve_range(p, b, &clipped);
-        for (int e = r.first + lane; e < r.last; e += 32) {
-            const int page = p.t.table[int64_t(b) * p.t.table_stride + e];
-            if (!entry_shared(p.t, page)) continue;
-            atomicAdd(&p.claims[page].here, 1u);
-            atomicMin(&p.claims[page].first, static_cast<unsigned long long>(b) << 32 | uint32_t(e));
-        }
-    }
-    // free pages of this CTA's share
-    int from, to;
-    pool_share(p.t.pages, rank, &from, &to);
-    int mine = 0;
-    for (int i = from + int(threadIdx.x); i < to; i += kPageThreads) mine += p.t.holders[i] == 0;
-    int found;
-    block_scan(mine, sums, &found);
-    if (threadIdx.x == 0) p.cta_free[rank] = found;
-    page_sync();
-    // what every request needs
-    for (int b = warp; b < p.t.requests; b += kWarps) {
-        const ReserveRange r = reserve_range(p, b, &clipped);
-        int leaves = 0;
-        bool copy = false;
-        for (int e = r.first + lane; e < r.last; e += 32) {
-            const int page = p.t.table[int64_t(b) * p.t.table_stride + e];
-            if (!entry_shared(p.t, page) || !entry_leaves(p, b, e, page)) continue;
-            ++leaves;
-            copy |= e == r.first && (r.start & ((1 << p.t.page_shift) - 1)) != 0;
-        }
-        leaves = __reduce_add_sync(0xffffffffu, leaves);
-        copy = __any_sync(0xffffffffu, copy);
-        if (lane == 0) {
-            p.fresh[b] = leaves + max(0, r.need - r.have);
-            p.copies[b] = copy;
-        }
-    }
-    page_sync();
-    // sums in front of each request (every CTA for itself; the first one keeps them), the lowest free pages in order
-    int64_t total = 0;                                        // (what is asked for may be more than there can be)
+    const ReserveRange mine = reserve_range(p, thread, &clipped);
+    auto range = [&](int round) { return round == 0 ? mine : reserve_range(p, thread + round * kAll, &clipped); };
+    auto shared = [&](int page) { return page >= 0 && page < p.t.pages && p.t.holders[page] > 1; };
+    auto order = [](int b, int e) { return static_cast<unsigned long long>(b) << 32 | uint32_t(e); };
+    // whether an entry gives its shared page up: another of those that are to write it keeps it, or somebody who is not
+    auto leaves = [&](int b, int e, int page) {
+        const PageClaim c = p.claims[page];
+        return !(int64_t(c.here) == p.t.holders[page] && c.first == order(b, e));
+    };
+
+    // free pages
+    uint32_t bits0 = 0;
+    int64_t there = 0, total = 0;                             // free pages, pages to be taken (cluster: added up below)
     int copies = 0;
-    for (int b0 = 0; b0 < p.t.requests; b0 += kPageThreads) {
-        const int b = b0 + int(threadIdx.x);
-        const int64_t n = b < p.t.requests ? p.fresh[b] : 0;
-        const int c = b < p.t.requests ? p.copies[b] : 0;
+    int place_first = 0;                                      // free pages of the first turn in front of the thread's, in its CTA
+    for (int k = 0; k < turns; ++k) {
+        const uint32_t bits = page_bits(p.t, (int64_t(k) * kAll + thread) * 32, false);
+        int found;
+        const int before = block_scan(__popc(bits), sums, &found);
+        if (k == 0) bits0 = bits, place_first = before;
+        there += found;
+        if (kCtas > 1 && threadIdx.x == 0) p.counts[k * kCtas + rank] = found;
+    }
+    // claims on shared pages: cleared, then counted
+    int any = 0;
+    for (int k = 0; k < rounds; ++k)
+        any |= for_entries(p.t, thread + k * kAll, range(k), [&](int, int, int page) {
+            bad |= page < 0 || page >= p.t.pages;
+            if (!shared(page)) return 0;
+            p.claims[page] = PageClaim{~0ull, 0u, 0u};
+            return 1;
+        });
+    // (without shared pages, as in most steps, there is nothing to count)
+    const bool claims = kCtas > 1 || __syncthreads_or(any) != 0;
+    if (claims) {
+        page_sync<kCtas>();
+        for (int k = 0; k < rounds; ++k)
+            for_entries(p.t, thread + k * kAll, range(k), [&](int b, int e, int page) {
+                if (!shared(page)) return 0;
+                atomicAdd(&p.claims[page].here, 1u);
+                atomicMin(&p.claims[page].first, order(b, e));
+                return 0;
+            });
+        page_sync<kCtas>();
+    }
+    // what every request needs, and the sums of it
+    int fresh0 = 0, copies0 = 0;                              // of the thread's first request
+    auto needs = [&](int k, int* copy) {
+        const ReserveRange r = range(k);
+        int first_leaves = 0;
+        const int gone = !claims ? 0 : for_entries(p.t, thread + k * kAll, r, [&](int b, int e, int page) { return int(shared(page) && leaves(b, e, page)); });
+        if (gone && r.line != 0) {
+            const int b = thread + k * kAll, page = p.t.table[int64_t(b) * p.t.table_stride + r.first];
+            first_leaves = shared(page) && leaves(b, r.first, page);
+        }
+        *copy = first_leaves;
+        return gone + max(0, r.need - r.have);
+    };
+    for (int k = 0; k < rounds; ++k) {
+        int copy, all_c;
+        const int64_t n = needs(k, &copy);
         int64_t all;
-        int all_c;
-        const int64_t before = total + block_scan(n, sums_wide, &all);
-        const int before_c = copies + block_scan(c, sums, &all_c);
+        const int64_t before = block_scan(n, sums_wide, &all);
+        const int before_c = block_scan(copy, sums, &all_c);
+        if (k == 0) fresh0 = int(min(before, int64_t(INT32_MAX))), copies0 = before_c;
         total += all;
         copies += all_c;
-        page_sync();                                       // (every CTA has read this part)
-        if (rank == 0 && b < p.t.requests) p.fresh[b] = int(min(before, int64_t(INT32_MAX))), p.copies[b] = before_c;
+        if (kCtas > 1 && threadIdx.x == 0) {
+            p.fresh[k * kCtas + rank] = int(min(all, int64_t(INT32_MAX)));
+            p.copies[k * kCtas + rank] = all_c;
+        }
     }
-    int at = 0, there = 0;
-    for (int c = 0; c < kPageCtas; ++c) {
-        const int f = p.cta_free[c];
-        if (c < rank) at += f;
-        there += f;
+    if (kCtas > 1) {
+        page_sync<kCtas>();
+        total = warp_sum(p.fresh, rounds * kCtas), there = warp_sum(p.counts, turns * kCtas);
+        copies = int(warp_sum(p.copies, rounds * kCtas));
     }
     const bool enough = there >= total;
-    for (int i0 = from; enough && i0 < to && at < total; i0 += kPageThreads) {
-        const int i = i0 + int(threadIdx.x);
-        const int f = i < to && p.t.holders[i] == 0;
-        int all;
-        const int place = at + block_scan(f, sums, &all);
-        if (f && place < total) p.free_list[place] = i;
-        at += all;
-    }
-    page_sync();
-    if (rank == 0 && threadIdx.x == 0) {
+    if (thread == 0) {
         *p.missing = enough ? 0 : int(min(total - there, int64_t(INT32_MAX)));
         *p.n_moves = enough ? copies : 0;
     }
+    // the lowest free pages, in order
+    int64_t passed = 0;                                       // free pages of the turns gone by (one CTA)
+    for (int k = 0; enough && k < turns; ++k) {
+        const int64_t base = kCtas > 1 ? warp_sum(p.counts, k * kCtas + rank) : passed;
+        if (base >= total) break;                             // (the same for the whole CTA)
+        const int64_t first = (int64_t(k) * kAll + thread) * 32;
+        uint32_t bits = bits0;
+        int64_t place = base + place_first;
+        if (k > 0 || turns > 1) {
+            int all;
+            if (k > 0) bits = page_bits(p.t, first, false);
+            place = base + block_scan(__popc(bits), sums, &all);
+            passed += all;
+        }
+        for (; bits && place < total; bits &= bits - 1) p.free_list[place++] = int(first) + __ffs(int(bits)) - 1;
+    }
+    page_sync<kCtas>();
     // (nothing above has changed the tables; holders of shared pages change when all entries have been decided on)
-    for (int b = warp; enough && b < p.t.requests; b += kWarps) {
-        const ReserveRange r = reserve_range(p, b, &clipped);
-        int place = p.fresh[b];
-        int32_t* const row = p.t.table + int64_t(b) * p.t.table_stride;
-        for (int e0 = min(r.first, r.have); e0 < r.need; e0 += 32) {
-            const int e = e0 + lane;
-            bool leave = false;
-            int page = -1;
-            if (e >= r.first && e < r.last) {
-                page = row[e];
-                leave = page >= 0 && page < p.t.pages && p.t.holders[page] > 1 && entry_leaves(p, b, e, page);
+    int64_t taken_before = 0;                                 // by the rounds gone by (one CTA)
+    int copied_before = 0;
+    for (int k = 0; enough && k < rounds; ++k) {
+        const ReserveRange r = range(k);
+        int copy = 0;
+        int64_t before = fresh0;
+        int before_c = copies0;
+        int64_t place0 = 0;
+        int move0 = 0;
+        if (kCtas > 1) place0 = warp_sum(p.fresh, k * kCtas + rank), move0 = int(warp_sum(p.copies, k * kCtas + rank));
+        else place0 = taken_before, move0 = copied_before;
+        if (k > 0 || rounds > 1) {
+            int all_c;
+            int64_t all;
+            const int64_t n = needs(k, &copy);
+            before = block_scan(n, sums_wide, &all);
+            before_c = block_scan(copy, sums, &all_c);
+            taken_before += all;
+            copied_before += all_c;
+        }
+        place0 += before;
+        move0 += before_c;
+        // one entry after the other by its request's lane, or (a prompt's pages) by the whole warp
+        const int b = thread + k * kAll, from = claims ? min(r.first, r.have) : r.have, n = max(r.need - from, 0);
+        auto take = [&](int b1, int e, int first, int last, int have, int64_t place, int page, bool leave, int line, int move) {
+            int32_t* const slot = p.free_list + place;
+            const int to = *slot;
+            *slot = leave ? page : -1;
+            if (leave && e == first && line != 0) {
+                int32_t* const m = p.moves + int64_t(move) * 3;
+                m[0] = page, m[1] = to, m[2] = line;
             }
-            const bool take = leave || (e >= r.have && e < r.need);
-            const uint32_t who = __ballot_sync(0xffffffffu, take);
-            if (take) {
-                int32_t* const line = p.free_list + place + __popc(who & ((1u << lane) - 1u));
-                const int to_page = *line;
-                *line = leave ? page : -1;
-                if (leave && e == r.first && (r.start & ((1 << p.t.page_shift) - 1)) != 0) {
-                    int32_t* const m = p.moves + int64_t(p.copies[b]) * 3;
-                    m[0] = page, m[1] = to_page, m[2] = r.start & ((1 << p.t.page_shift) - 1);
-                }
-                row[e] = to_page;
-                p.t.holders[to_page] = 1;
+            p.t.table[int64_t(b1) * p.t.table_stride + e] = to;
+            p.t.holders[to] = 1;
+        };
+        auto leaving = [&](int b1, int e, int first, int last, int* page) {
+            if (!claims || e < first || e >= last) return false;
+            *page = p.t.table[int64_t(b1) * p.t.table_stride + e];
+            return shared(*page) && leaves(b1, e, *page);
+        };
+        constexpr int kFew = 2;
+        if (n <= kFew) {
+            int64_t place = place0;
+            for (int e = from; e < r.need; ++e) {
+                int page = -1;
+                const bool leave = leaving(b, e, r.first, r.last, &page);
+                if (leave || e >= r.have) take(b, e, r.first, r.last, r.have, place++, page, leave, r.line, move0);
             }
-            place += __popc(who);
         }
         __syncwarp();
-        if (lane == 0 && p.t.held[b] < r.need) p.t.held[b] = r.need;
+        for (uint32_t many = __ballot_sync(0xffffffffu, n > kFew); many; many &= many - 1) {
+            const int l = __ffs(int(many)) - 1, b1 = __shfl_sync(0xffffffffu, b, l), need = __shfl_sync(0xffffffffu, r.need, l);
+            const int first = __shfl_sync(0xffffffffu, r.first, l), last = __shfl_sync(0xffffffffu, r.last, l);
+            const int have = __shfl_sync(0xffffffffu, r.have, l), line = __shfl_sync(0xffffffffu, r.line, l);
+            const int move = __shfl_sync(0xffffffffu, move0, l);
+            int64_t place = __shfl_sync(0xffffffffu, place0, l);
+            for (int e0 = __shfl_sync(0xffffffffu, from, l); e0 < need; e0 += 32) {
+                const int e = e0 + lane;
+                int page = -1;
+                const bool leave = leaving(b1, e, first, last, &page), taken = leave || (e >= have && e < need);
+                const uint32_t who = __ballot_sync(0xffffffffu, taken);
+                if (taken) take(b1, e, first, last, have, place + __popc(who & ((1u << lane) - 1u)), page, leave, line, move);
+                place += __popc(who);
+            }
+        }
+        if (r.need > r.have) p.t.held[b] = r.need;
     }
-    page_sync();
-    for (int i = rank * kPageThreads + int(threadIdx.x); enough && i < total; i += kPageCtas * kPageThreads)
-        if (p.free_list[i] >= 0) atomicSub(&p.t.holders[p.free_list[i]], 1);
+    if (claims) {
+        page_sync<kCtas>();
+        for (int64_t i = thread; enough && i < total; i += kAll)
+            if (p.free_list[i] >= 0) atomicSub(&p.t.holders[p.free_list[i]], 1);
+    }
     if (clipped || bad) atomicCAS(p.status, 0u, kBadPage);
 }
 
@@ -245,11 +344,22 @@ __global__ void __launch_bounds__(256) page_release_kernel(const PageView t, con
     const int kept = int(min((int64_t(keep) + (1 << t.page_shift) - 1) >> t.page_shift, int64_t(have)));
     int32_t* const row = t.table + int64_t(b) * t.table_stride;
     bool bad = false;
-    for (int e = kept + int(lane_id()); e < have; e += 32) {
-        const int page = row[e];
-        row[e] = -1;
-        if (page < 0 || page >= t.pages) bad = true;
-        else if (atomicSub(&t.holders[page], 1) <= 0) atomicAdd(&t.holders[page], 1), bad = true;
+    constexpr int kAhead = 4;
+    for (int e0 = kept + int(lane_id()); e0 < have; e0 += 32 * kAhead) {
+        int page[kAhead], had[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) page[k] = e0 + 32 * k < have ? row[e0 + 32 * k] : 0;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            had[k] = 1;
+            if (e0 + 32 * k >= have) continue;
+            row[e0 + 32 * k] = -1;
+            if (page[k] < 0 || page[k] >= t.pages) bad = true;
+            else had[k] = atomicSub(&t.holders[page[k]], 1);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (had[k] <= 0) atomicAdd(&t.holders[page[k]], 1), bad = true;           // (it had no holder)
     }
     __syncwarp();
     if (lane_id() == 0) t.held[b] = kept;
@@ -265,14 +375,13 @@ struct ForkParams {
     int forks;
     uint32_t* status;
 };
-__global__ void __cluster_dims__(kPageCtas, 1, 1) __launch_bounds__(kPageThreads) page_fork_kernel(const ForkParams p) {
+// Which forks are made, and how many pages each shares; `held` is that after the call.  One CTA: every count is read before one is
+// written.
+__global__ void __launch_bounds__(kPageThreads) page_fork_kernel(const ForkParams p) {
     pdl_wait();
     pdl_launch_dependents();
-    const int rank = int(cluster_cta_rank()), lane = int(lane_id());
-    constexpr int kAll = kPageCtas * kPageThreads;
-    const int thread = rank * kPageThreads + int(threadIdx.x), warp = thread / 32;
-    bool refused = false, bad = false;
-    for (int f = thread; f < p.forks; f += kAll) {
+    bool refused = false;
+    for (int f = int(threadIdx.x); f < p.forks; f += kPageThreads) {
         const int from = p.from[f], to = p.to[f];
         int n = -1;
         if (from >= 0 && from < p.t.requests && to >= 0 && to < p.t.requests && p.t.held[to] == 0) {
@@ -281,31 +390,37 @@ __global__ void __cluster_dims__(kPageCtas, 1, 1) __launch_bounds__(kPageThreads
         }
         p.entries[f] = n;
     }
-    page_sync();
+    __syncthreads();
     // of several forks to one request the first has it: the lowest of their marks, which are negative
-    for (int f = thread; f < p.forks; f += kAll)
+    for (int f = int(threadIdx.x); f < p.forks; f += kPageThreads)
         if (p.entries[f] >= 0) atomicMin(&p.t.held[p.to[f]], f - p.forks);
-    page_sync();
-    for (int f = thread; f < p.forks; f += kAll) {
-        if (p.entries[f] >= 0 && p.t.held[p.to[f]] != f - p.forks) p.entries[f] = -1;
+    __syncthreads();
+    for (int f = int(threadIdx.x); f < p.forks; f += kPageThreads) {
+        if (p.entries[f] >= 0 && *static_cast<volatile int32_t*>(&p.t.held[p.to[f]]) != f - p.forks) p.entries[f] = -1;
         refused |= p.entries[f] < 0;
     }
-    page_sync();
-    // (a request that is forked to holds nothing, so no row is read that is written here)
-    for (int f = warp; f < p.forks; f += kAll / 32) {
-        const int n = p.entries[f];
-        if (n < 0) continue;
-        const int32_t* const src = p.t.table + int64_t(p.from[f]) * p.t.table_stride;
-        int32_t* const dst = p.t.table + int64_t(p.to[f]) * p.t.table_stride;
-        for (int e = lane; e < n; e += 32) {
-            const int page = src[e];
-            dst[e] = page;
-            if (page < 0 || page >= p.t.pages) bad = true;
-            else atomicAdd(&p.t.holders[page], 1);
-        }
-        if (lane == 0) p.t.held[p.to[f]] = n;
-    }
+    __syncthreads();
+    for (int f = int(threadIdx.x); f < p.forks; f += kPageThreads)
+        if (p.entries[f] >= 0) p.t.held[p.to[f]] = p.entries[f];
     if (refused) atomicCAS(p.status, 0u, kBadFork);
+}
+// A warp per fork.  (A request that is forked to held nothing, so no row is read that is written here.)
+__global__ void __launch_bounds__(256) page_share_kernel(const ForkParams p) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int f = int(blockIdx.x) * 8 + int(threadIdx.x) / 32;
+    if (f >= p.forks) return;
+    const int n = p.entries[f];
+    if (n <= 0) return;
+    const int32_t* const src = p.t.table + int64_t(p.from[f]) * p.t.table_stride;
+    int32_t* const dst = p.t.table + int64_t(p.to[f]) * p.t.table_stride;
+    bool bad = false;
+    for (int e = int(lane_id()); e < n; e += 32) {
+        const int page = src[e];
+        dst[e] = page;
+        if (page < 0 || page >= p.t.pages) bad = true;
+        else atomicAdd(&p.t.holders[page], 1);
+    }
     if (bad) atomicCAS(p.status, 0u, kBadPage);
 }
 
@@ -315,61 +430,76 @@ struct CompactParams {
     int32_t* n_moves;
     int32_t* in_use;
     int32_t* went;                       // [pages]: where a page behind the last one in use went (itself: nowhere)
-    int32_t* cta_live;                   // [kPageCtas]: pages in use in each CTA's share; then the moves, then all pages in use
+    int32_t* counts;                     // [turns of the pool * CTAs]: pages in use
+    int32_t* sums;                       // [2]: pages in use, free places in front of that number
     int most;
     uint32_t* status;
 };
-__global__ void __cluster_dims__(kPageCtas, 1, 1) __launch_bounds__(kPageThreads) page_compact_kernel(const CompactParams p) {
+template <int kCtas>
+__global__ void __launch_bounds__(kPageThreads) page_compact_kernel(const CompactParams p) {
     __shared__ int sums[kPageWarps];
     pdl_wait();
     pdl_launch_dependents();
-    const int rank = int(cluster_cta_rank());
-    int from, to;
-    pool_share(p.t.pages, rank, &from, &to);
-    int mine = 0;
-    for (int i = from + int(threadIdx.x); i < to; i += kPageThreads) mine += p.t.holders[i] > 0;
-    int found;
-    block_scan(mine, sums, &found);
-    if (threadIdx.x == 0) p.cta_live[rank] = found;
-    page_sync();
-    int live = 0, before = 0;
-    for (int c = 0; c < kPageCtas; ++c) {
-        const int n = p.cta_live[c];
-        if (c < rank) before += n;
-        live += n;
+    const int rank = kCtas > 1 ? int(cluster_cta_rank()) : 0;
+    constexpr int kAll = kCtas * kPageThreads;
+    const int thread = rank * kPageThreads + int(threadIdx.x);
+    const int turns = int((int64_t(p.t.pages) + kAll * 32 - 1) / (kAll * 32));
+    uint32_t bits0 = 0;
+    int live = 0, passed = 0;
+    for (int k = 0; k < turns; ++k) {
+        const uint32_t bits = page_bits(p.t, (int64_t(k) * kAll + thread) * 32, true);
+        if (k == 0) bits0 = bits;
+        int found;
+        block_scan(__popc(bits), sums, &found);
+        live += found;
+        if (kCtas > 1 && threadIdx.x == 0) p.counts[k * kCtas + rank] = found;
+    }
+    if (kCtas > 1) {
+        page_sync<kCtas>();
+        live = int(warp_sum(p.counts, turns * kCtas));
     }
     // Pages in use from `live` on, the highest first, and free places in front of it, the lowest first: as many of one as of the
     // other.
-    for (int i0 = from; i0 < to; i0 += kPageThreads) {
-        const int i = i0 + int(threadIdx.x);
-        const int used = i < to && p.t.holders[i] > 0;
+    if (live == 0 && thread == 0) p.sums[1] = 0;
+    for (int k = 0; k < turns; ++k) {
+        const int64_t first = (int64_t(k) * kAll + thread) * 32;
+        const uint32_t bits = k == 0 ? bits0 : page_bits(p.t, first, true);
         int all;
-        const int in_front = before + block_scan(used, sums, &all);
-        before += all;
-        if (i >= to) continue;
-        if (i == live - 1) p.cta_live[kPageCtas] = live - in_front - used;       // places in front of `live` that are free
-        if (i < live && !used) {
-            const int r = i - in_front;
-            if (r < p.most) p.moves[int64_t(r) * 3 + 1] = i;
-        } else if (i >= live) {
-            const int r = live - 1 - in_front;
-            if (used && r < p.most) p.moves[int64_t(r) * 3] = i;
-            p.went[i] = i;
+        const int before = (kCtas > 1 ? int(warp_sum(p.counts, k * kCtas + rank)) : passed) + block_scan(__popc(bits), sums, &all);
+        passed += all;
+        const int lane = int(lane_id());
+        const int64_t base = first - int64_t(lane) * 32;
+        for (int j = 0; j < 32 && base + j * 32 < p.t.pages; ++j) {             // one thread's pages side by side
+            const uint32_t word = __shfl_sync(0xffffffffu, bits, j);
+            const int in_front = __shfl_sync(0xffffffffu, before, j) + __popc(word & ((1u << lane) - 1u));
+            if (base + j * 32 + lane >= p.t.pages) continue;
+            const int i = int(base) + j * 32 + lane;
+            const int used = int(word >> lane & 1u);
+            if (i < live && !used) {
+                const int r = i - in_front;
+                if (r < p.most) p.moves[int64_t(r) * 3 + 1] = i;
+            } else if (i >= live) {
+                const int r = live - 1 - in_front;
+                if (used && r < p.most) p.moves[int64_t(r) * 3] = i;
+                p.went[i] = i;
+            }
+            if (i == live - 1) p.sums[1] = live - in_front - used;
         }
+        __syncwarp();
     }
-    page_sync();
-    const int moves = min(live == 0 ? 0 : p.cta_live[kPageCtas], p.most);
-    for (int r = rank * kPageThreads + int(threadIdx.x); r < moves; r += kPageCtas * kPageThreads) {
+    page_sync<kCtas>();
+    const int moves = min(p.sums[1], p.most);
+    for (int r = thread; r < moves; r += kAll) {
         const int a = p.moves[int64_t(r) * 3], b = p.moves[int64_t(r) * 3 + 1];
         p.moves[int64_t(r) * 3 + 2] = 1 << p.t.page_shift;
         p.went[a] = b;
         p.t.holders[b] = p.t.holders[a];
         p.t.holders[a] = 0;
     }
-    if (rank == 0 && threadIdx.x == 0) {
+    if (thread == 0) {
         *p.n_moves = moves;
         *p.in_use = live;
-        p.cta_live[kPageCtas + 1] = live;
+        p.sums[0] = live;
     }
 }
 
@@ -465,9 +595,37 @@ static int page_view(const tl_page_tables* t, PageView* out) {
 }
 
 static size_t up16(size_t n) { return (n + 15) / 16 * 16; }
+// Sizes of the lists that reserving and compacting keep per CTA and turn (those of the cluster are the longer ones).
+static size_t page_turns(int64_t n, int64_t each) { return up16(size_t(ceil_div(n, kPageThreads * each)) * 4 + kPageCtas * 4); }
 static size_t page_workspace(const PageView& t, int forks) {
-    const size_t reserve = up16(size_t(t.pages) * sizeof(PageClaim)) + up16(size_t(t.requests) * 4) * 2 + up16(size_t(t.pages) * 4) + 256;
-    return std::max(reserve, up16(size_t(forks) * 4));        // (compacting takes less than reserving)
+    const size_t reserve = up16(size_t(t.pages) * sizeof(PageClaim)) + up16(size_t(t.pages) * 4) + page_turns(t.pages, 32) + 2 * page_turns(t.requests, 1);
+    const size_t compact = up16(size_t(t.pages) * 4) + page_turns(t.pages, 32) + 16;
+    return std::max(std::max(reserve, compact), up16(size_t(forks) * 4));
+}
+
+// A kernel that looks through the pool: one CTA, or a cluster.
+template <typename P>
+static int page_launch(const PageView& t, void (*one)(P), void (*cluster)(P), const P& p, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    const bool single = t.pages <= kPagesOfOne;
+    cfg.gridDim = dim3(single ? 1 : kPageCtas);
+    cfg.blockDim = dim3(kPageThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (!single) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = kPageCtas, attr[n].val.clusterDim.y = 1, attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (opt(TL_OPT_PDL) != 0) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = unsigned(n);
+    return check_cuda(cudaLaunchKernelEx(&cfg, single ? one : cluster, p));
 }
 
 }  // namespace tl
@@ -496,17 +654,17 @@ int tl_page_reserve(const tl_page_tables* tables, const int32_t* d_start, const 
     if (int rc = get_workspace(page_workspace(p.t, 0), &ws, stream)) return rc;
     char* at = static_cast<char*>(ws);
     p.claims = reinterpret_cast<PageClaim*>(at), at += up16(size_t(p.t.pages) * sizeof(PageClaim));
-    p.fresh = reinterpret_cast<int32_t*>(at), at += up16(size_t(p.t.requests) * 4);
-    p.copies = reinterpret_cast<int32_t*>(at), at += up16(size_t(p.t.requests) * 4);
     p.free_list = reinterpret_cast<int32_t*>(at), at += up16(size_t(p.t.pages) * 4);
-    p.cta_free = reinterpret_cast<int32_t*>(at);
+    p.counts = reinterpret_cast<int32_t*>(at), at += page_turns(p.t.pages, 32);
+    p.fresh = reinterpret_cast<int32_t*>(at), at += page_turns(p.t.requests, 1);
+    p.copies = reinterpret_cast<int32_t*>(at);
     p.start = d_start;
     p.tokens = d_tokens;
     p.moves = d_moves;
     p.n_moves = d_n_moves;
     p.missing = d_missing;
     p.status = dev().ctl.d_status;
-    return kv_launch(page_reserve_kernel, dim3(kPageCtas), kPageThreads, stream, p);
+    return page_launch(p.t, page_reserve_kernel<1>, page_reserve_kernel<kPageCtas>, p, stream);
 }
 
 int tl_page_release(const tl_page_tables* tables, const int32_t* d_tokens, void* cuda_stream) {
@@ -542,7 +700,8 @@ int tl_page_fork(const tl_page_tables* tables, const int32_t* d_from, const int3
     p.entries = static_cast<int32_t*>(ws);
     p.forks = forks;
     p.status = dev().ctl.d_status;
-    return kv_launch(page_fork_kernel, dim3(kPageCtas), kPageThreads, stream, p);
+    if (int rc = kv_launch(page_fork_kernel, dim3(1), kPageThreads, stream, p)) return rc;
+    return kv_launch(page_share_kernel, dim3(unsigned(ceil_div(forks, 8))), 256, stream, p);
 }
 
 int tl_page_compact(const tl_page_tables* tables, int32_t* d_moves, int most, int32_t* d_n_moves, int32_t* d_in_use, void* cuda_stream) {
@@ -558,16 +717,17 @@ int tl_page_compact(const tl_page_tables* tables, int32_t* d_moves, int most, in
     void* ws = nullptr;
     if (int rc = get_workspace(page_workspace(p.t, 0), &ws, stream)) return rc;
     p.went = static_cast<int32_t*>(ws);
-    p.cta_live = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + up16(size_t(p.t.pages) * 4));
+    p.counts = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + up16(size_t(p.t.pages) * 4));
+    p.sums = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(p.counts) + page_turns(p.t.pages, 32));
     p.moves = d_moves;
     p.n_moves = d_n_moves;
     p.in_use = d_in_use;
     p.most = most;
     p.status = dev().ctl.d_status;
-    if (int rc = kv_launch(page_compact_kernel, dim3(kPageCtas), kPageThreads, stream, p)) return rc;
+    if (int rc = page_launch(p.t, page_compact_kernel<1>, page_compact_kernel<kPageCtas>, p, stream)) return rc;
     if (p.t.requests == 0) return TL_OK;
     return kv_launch(page_rename_kernel, dim3(unsigned(ceil_div(p.t.requests, 8))), 256, stream, p.t, const_cast<const int32_t*>(p.went),
-                     const_cast<const int32_t*>(p.cta_live + kPageCtas + 1), p.status);
+                     const_cast<const int32_t*>(p.sums), p.status);
 }
 
 int tl_page_copy(const tl_kv_cache* from, const tl_kv_cache* to, const int32_t* d_moves, const int32_t* d_n_moves, int most,
