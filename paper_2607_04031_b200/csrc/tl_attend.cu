@@ -123,7 +123,7 @@ static int attend_plan(const tl_kv_cache* cache, const tl_kv_batch* batch, int q
     const int64_t room = std::min(batch->table_stride * cache->page_tokens, kKvMaxTokens);
     int64_t sms = dev().sm_count;
     if (opt(TL_OPT_SM_LIMIT) > 0) sms = std::min(sms, opt(TL_OPT_SM_LIMIT));
-    if (cache->head_dim <= 128 && rows > (cache->head_dim == 128 ? 24 : 32)) {
+    if (cache->head_dim <= 128 && rows > (cache->head_dim == 128 && cache->format != TL_KV_E2M1 ? 24 : 32)) {
         plan->tile_tokens = 128;
         plan->ctas_per_sm = 1;
         const double positions = std::min(double(batch->requests) * double(room), double(cache->pages) * cache->page_tokens);

@@ -172,27 +172,192 @@ __global__ void __launch_bounds__(kCopyThreads) kv_read_kernel(const KvCopyParam
         using Codes = typename KvCodes<kFmt>::type;
         Codes c[kCopyAhead];
         float s[kCopyAhead];
-        uint32_t g[kCopyAhead];
 #pragma unroll
         for (int i = 0; i < kCopyAhead; ++i) {
             const int head = head0 + i * kPerWarp;
             c[i] = Codes{};
             s[i] = 0.0f;
-            g[i] = 0;
             if (head >= heads || !at.page) continue;
             c[i] = *reinterpret_cast<const Codes*>(p.cache.base[which] + at.at + int64_t(head) * p.cache.head_stride + l * int(sizeof(Codes)));
             if (kFmt != TL_KV_BF16) s[i] = p.cache.scale[which][at.scale_at + int64_t(head) * p.cache.scale_head_stride];
-            if (kFmt == TL_KV_E2M1) g[i] = uint8_t(p.cache.group[which][at.group_at + int64_t(head) * p.cache.group_head_stride + (l >> 1)]);
         }
         char* const dst = p.rows[which] + int64_t(row) * p.row_stride + (int64_t(head0) * kDim + l * 8) * kItem;
 #pragma unroll
         for (int i = 0; i < kCopyAhead; ++i) {
             if (head0 + i * kPerWarp >= heads) continue;
             float x[8];
-            if constexpr (kFmt == TL_KV_E2M1) KvCodes<kFmt>::expand(c[i], group_f16x2(g[i], 0, 0, 0), s[i], x);
-            else KvCodes<kFmt>::expand(c[i], s[i], x);
+            KvCodes<kFmt>::expand(c[i], s[i], x);
             store8(dst + int64_t(i) * kPerWarp * kDim * kItem, kF32, x);
         }
+    }
+}
+
+// The same two for 4-bit caches.  A lane owns the 16 elements of a group scale (32 bytes of bf16, 8 of codes), a group of kDim / 16
+// lanes a row's head, and a warp several neighbouring rows, whose places are looked up together: with 4 bits a row of 8 heads is
+// 512 bytes, too little for a warp to wait for alone.  8192 rows of 8 heads x 128 appended and 26000 read back, from and to bf16, one row
+// per warp and eight elements per lane: 55 us.
+// Heads per warp, whole call of the above: 8 read and 4 appended at a time 50 us, 4 and 4 48, 4 and 2 46, 2 and 2 50.
+constexpr int kFourHeads = 4, kFourAppendHeads = 2, kFourReadCtas = 4;
+
+// 32 bytes at once where they are aligned so.
+__device__ __forceinline__ void load32(const char* src, bool wide, uint32_t (&v)[8]) {
+    if (wide) {
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(src));
+    } else {
+        const uint4 a = *reinterpret_cast<const uint4*>(src), b = *reinterpret_cast<const uint4*>(src + 16);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    }
+}
+__device__ __forceinline__ void store32(char* dst, bool wide, const uint32_t (&v)[8]) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                     ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "l"(dst) : "memory");
+    } else {
+        *reinterpret_cast<uint4*>(dst) = make_uint4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<uint4*>(dst + 16) = make_uint4(v[4], v[5], v[6], v[7]);
+    }
+}
+
+// Where the lane's row lies, for rows base + lane / (32 / kRows) of a warp.  False: no request owns it.
+template <int kRows>
+__device__ __forceinline__ bool kv_locate_rows(const KvView& cache, const KvBatchView& bv, int base, int groups, KvRowPlace* out) {
+    const int sub = int(lane_id()) / (32 / kRows), row = base + sub;
+    int b = -1, first = 0, start = 0;
+    for (int b0 = 0; b0 < bv.requests; b0 += 32) {
+        const int mine = min(b0 + int(lane_id()), bv.requests - 1);
+        const KvRequest q = kv_request(bv, cache.page_shift, mine);
+        uint32_t found = 0;                                   // of the lane's row
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const uint32_t owner = __ballot_sync(0xffffffffu, b0 + int(lane_id()) < bv.requests && base + r >= q.first && base + r < q.first + q.n);
+            if (r == sub) found = owner;
+        }
+        const int l = found ? __ffs(int(found)) - 1 : 0;
+        const int f = __shfl_sync(0xffffffffu, q.first, l), st = __shfl_sync(0xffffffffu, q.start, l);
+        if (found) b = b0 + l, first = f, start = st;
+        if (__all_sync(0xffffffffu, b >= 0)) break;
+    }
+    out->page = false;
+    out->pos = start + (row - first);
+    out->at = out->scale_at = out->group_at = 0;
+    if (b < 0) return false;
+    if (out->pos >= kv_room(bv, cache.page_shift)) return true;
+    const int64_t page = bv.page_table[int64_t(b) * bv.table_stride + (out->pos >> cache.page_shift)];
+    const int line = out->pos & ((1 << cache.page_shift) - 1);
+    out->page = page >= 0 && page < cache.pages;
+    if (!out->page) return true;
+    out->at = page * cache.page_stride + line * cache.token_stride;
+    out->scale_at = page * cache.scale_page_stride + line;
+    out->group_at = page * cache.group_page_stride + line * groups;
+    return true;
+}
+
+template <int kDim, bool kF32>
+__global__ void __launch_bounds__(kCopyThreads) kv_four_append_kernel(const KvCopyParams p) {
+    pdl_wait();
+    pdl_launch_dependents();
+    constexpr int kLanes = kDim / 16, kRows = 32 / kLanes, kItem = kF32 ? 4 : 2, kWords = kF32 ? 2 : 1;
+    const int which = int(blockIdx.y) & 1, head0 = int(blockIdx.y >> 1) * kFourAppendHeads, heads = min(p.cache.heads - head0, kFourAppendHeads);
+    const int sub = int(lane_id()) / kLanes, l = int(lane_id()) % kLanes;
+    const bool wide = ((reinterpret_cast<uintptr_t>(p.rows[which]) | uintptr_t(p.row_stride)) & 31u) == 0;
+    const int64_t step = int64_t(gridDim.x) * (kCopyThreads / 32) * kRows;
+    for (int64_t base = (blockIdx.x * int64_t(kCopyThreads / 32) + threadIdx.x / 32) * kRows; base < p.batch.tokens; base += step) {
+        const int64_t row = base + sub;
+        const char* const src = p.rows[which] + (row < p.batch.tokens ? row : base) * p.row_stride + (int64_t(head0) * kDim + l * 16) * kItem;
+        uint32_t raw[kFourAppendHeads][kWords][8];
+#pragma unroll
+        for (int i = 0; i < kFourAppendHeads; ++i)
+#pragma unroll
+            for (int w = 0; w < kWords; ++w)
+                if (i < heads) load32(src + int64_t(i) * kDim * kItem + w * 32, wide, raw[i][w]);
+        KvRowPlace at;
+        const bool owned = kv_locate_rows<kRows>(p.cache, p.batch, int(base), kDim / 16, &at) && row < p.batch.tokens;
+        if (owned && !at.page && l == 0) atomicCAS(p.status, 0u, kBadPage);
+        const bool write = owned && at.page;
+#pragma unroll
+        for (int i = 0; i < kFourAppendHeads; ++i) {
+            if (i >= heads) continue;
+            float x[2][8];
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (kF32) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[k][e] = __uint_as_float(raw[i][kF32 ? k : 0][e]);
+                    top = max(top, kv_top_f32(x[k]));
+                } else {
+                    const uint4 v = make_uint4(raw[i][0][4 * k], raw[i][0][4 * k + 1], raw[i][0][4 * k + 2], raw[i][0][4 * k + 3]);
+                    load8(reinterpret_cast<const char*>(&v), false, x[k]);
+                    top = max(top, kv_top_bf16(v));
+                }
+            }
+            uint32_t row_top = top;
+#pragma unroll
+            for (int d = kLanes / 2; d > 0; d >>= 1) row_top = max(row_top, __shfl_xor_sync(0xffffffffu, row_top, d));
+            const E2m1Row r = e2m1_row(row_top);
+            const uint32_t byte = e2m1_group(top, r), lo = e2m1_codes(x[0], byte, r), hi = e2m1_codes(x[1], byte, r);
+            if (!write) continue;
+            const int64_t head = head0 + i;
+            *reinterpret_cast<uint2*>(p.cache.base[which] + at.at + head * p.cache.head_stride + l * 8) = make_uint2(lo, hi);
+            p.cache.group[which][at.group_at + head * p.cache.group_head_stride + l] = char(byte);
+            if (l == 0) p.cache.scale[which][at.scale_at + head * p.cache.scale_head_stride] = r.scale;
+        }
+    }
+}
+
+// (The next rows' places are looked up while these rows' codes are on their way.)
+template <int kDim, bool kF32>
+__global__ void __launch_bounds__(kCopyThreads, kFourReadCtas) kv_four_read_kernel(const KvCopyParams p) {
+    pdl_wait();
+    pdl_launch_dependents();
+    constexpr int kLanes = kDim / 16, kRows = 32 / kLanes, kItem = kF32 ? 4 : 2;
+    const int which = int(blockIdx.y) & 1, head0 = int(blockIdx.y >> 1) * kFourHeads, heads = min(p.cache.heads - head0, kFourHeads);
+    const int sub = int(lane_id()) / kLanes, l = int(lane_id()) % kLanes;
+    const bool wide = ((reinterpret_cast<uintptr_t>(p.rows[which]) | uintptr_t(p.row_stride)) & 31u) == 0;
+    const int64_t step = int64_t(gridDim.x) * (kCopyThreads / 32) * kRows;
+    int64_t base = (blockIdx.x * int64_t(kCopyThreads / 32) + threadIdx.x / 32) * kRows;
+    if (base >= p.batch.tokens) return;
+    KvRowPlace at;
+    bool owned = kv_locate_rows<kRows>(p.cache, p.batch, int(base), kDim / 16, &at);
+    while (true) {
+        const int64_t row = base + sub;
+        const bool here = owned && row < p.batch.tokens, page = here && at.page;
+        if (here && !page && l == 0) atomicCAS(p.status, 0u, kBadPage);
+        const char* const codes = p.cache.base[which] + at.at + int64_t(head0) * p.cache.head_stride + l * 8;
+        const char* const group = p.cache.group[which] + at.group_at + int64_t(head0) * p.cache.group_head_stride + l;
+        const float* const scale = p.cache.scale[which] + at.scale_at + int64_t(head0) * p.cache.scale_head_stride;
+        uint2 c[kFourHeads];
+        uint32_t g[kFourHeads];
+        float s[kFourHeads];
+#pragma unroll
+        for (int i = 0; i < kFourHeads; ++i) {
+            c[i] = make_uint2(0, 0), g[i] = 0, s[i] = 0.0f;
+            if (i >= heads || !page) continue;
+            c[i] = *reinterpret_cast<const uint2*>(codes + i * p.cache.head_stride);
+            g[i] = uint8_t(group[i * p.cache.group_head_stride]);
+            s[i] = scale[i * p.cache.scale_head_stride];
+        }
+        base += step;
+        const bool more = base < p.batch.tokens;
+        if (more) owned = kv_locate_rows<kRows>(p.cache, p.batch, int(base), kDim / 16, &at);
+        char* const dst = p.rows[which] + row * p.row_stride + (int64_t(head0) * kDim + l * 16) * kItem;
+#pragma unroll
+        for (int i = 0; i < kFourHeads; ++i) {
+            if (i >= heads || !here) continue;
+            float x[2][8];
+            const uint32_t g2 = group_f16x2(g[i], 0, 0, 0);
+            KvCodes<TL_KV_E2M1>::expand(c[i].x, g2, s[i], x[0]);
+            KvCodes<TL_KV_E2M1>::expand(c[i].y, g2, s[i], x[1]);
+            uint32_t v[8];
+#pragma unroll
+            for (int w = 0; w < (kF32 ? 2 : 1); ++w) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = kF32 ? __float_as_uint(x[w][e]) : pack_bf16(x[e / 4][e % 4 * 2], x[e / 4][e % 4 * 2 + 1]);
+                store32(dst + int64_t(i) * kDim * kItem + w * 32, wide, v);
+            }
+        }
+        if (!more) break;
     }
 }
 
@@ -305,6 +470,15 @@ static CopyKernel pick_copy(bool append, int dim) {
     }
 }
 
+template <bool kF32>
+static CopyKernel pick_four(bool append, int dim) {
+    switch (dim) {
+        case 64: return append ? kv_four_append_kernel<64, kF32> : kv_four_read_kernel<64, kF32>;
+        case 128: return append ? kv_four_append_kernel<128, kF32> : kv_four_read_kernel<128, kF32>;
+        default: return append ? kv_four_append_kernel<256, kF32> : kv_four_read_kernel<256, kF32>;
+    }
+}
+
 static int kv_copy(bool append, const tl_kv_cache* cache, const tl_kv_batch* batch, const void* k, const void* v, int elem,
                    int64_t row_stride, void* cuda_stream) {
     KvCopyParams p = {};
@@ -327,12 +501,15 @@ static int kv_copy(bool append, const tl_kv_cache* cache, const tl_kv_batch* bat
     switch (cache->format) {
         case TL_KV_BF16: kernel = f32 ? pick_copy<TL_KV_BF16, true>(append, cache->head_dim) : pick_copy<TL_KV_BF16, false>(append, cache->head_dim); break;
         case TL_KV_E4M3: kernel = f32 ? pick_copy<TL_KV_E4M3, true>(append, cache->head_dim) : pick_copy<TL_KV_E4M3, false>(append, cache->head_dim); break;
-        case TL_KV_E2M1: kernel = f32 ? pick_copy<TL_KV_E2M1, true>(append, cache->head_dim) : pick_copy<TL_KV_E2M1, false>(append, cache->head_dim); break;
+        case TL_KV_E2M1: kernel = f32 ? pick_four<true>(append, cache->head_dim) : pick_four<false>(append, cache->head_dim); break;
         default: kernel = f32 ? pick_copy<TL_KV_INT8, true>(append, cache->head_dim) : pick_copy<TL_KV_INT8, false>(append, cache->head_dim); break;
     }
-    const int64_t chunks = ceil_div(cache->heads, int64_t(kCopyAhead) * (32 / (cache->head_dim / 8)));
+    const bool four = cache->format == TL_KV_E2M1;
+    const int64_t chunks = four ? ceil_div(cache->heads, append ? kFourAppendHeads : kFourHeads) : ceil_div(cache->heads, int64_t(kCopyAhead) * (32 / (cache->head_dim / 8)));
     if (2 * chunks > 65535) return TL_ERR_UNSUPPORTED;
-    const int64_t blocks = std::min<int64_t>(ceil_div(p.batch.tokens, kCopyThreads / 32), std::max<int64_t>(int64_t(dev().sm_count) * 16 / chunks, 1));
+    const int64_t rows = kCopyThreads / 32 * int64_t(four ? 512 / cache->head_dim : 1);                  // of a block at a time
+    const int64_t most = four && !append ? int64_t(dev().sm_count) * kFourReadCtas / (2 * chunks) : int64_t(dev().sm_count) * 16 / chunks;
+    const int64_t blocks = std::min<int64_t>(ceil_div(p.batch.tokens, rows), std::max<int64_t>(most, 1));
     return kv_launch(kernel, dim3(unsigned(blocks), unsigned(2 * chunks)), kCopyThreads, static_cast<cudaStream_t>(cuda_stream), p);
 }
 

@@ -136,6 +136,43 @@ __device__ __forceinline__ uint32_t kv_top_bf16(const uint4& v) {
     for (int e = 0; e < 4; ++e) top = __vmaxu2(top, u[e] & 0x7fff7fffu);                          // two bf16 patterns at a time
     return max(top & 0xffff0000u, top << 16);
 }
+// The 4-bit format's rule, in three steps: the row's scale from its largest magnitude (as bits), a group's from its own, codes.
+struct E2m1Row {
+    float scale, to;                     // and 1 / scale (exact); 0 where every code is 0
+};
+__device__ __forceinline__ E2m1Row e2m1_row(uint32_t top) {
+    const bool finite = top < 0x7f800000u, some = finite && top != 0;
+    // the least power of two of which 6 * 448 = 1.3125 * 2^11 times is not below the largest magnitude
+    const int k = max(int(top >> 23) - 138 + ((top & 0x7fffffu) > 0x280000u ? 1 : 0), -126);
+    return {some ? __uint_as_float(uint32_t(k + 127) << 23) : finite ? 0.0f : __uint_as_float(0x7fc00000u),
+            some ? __uint_as_float(uint32_t(127 - k) << 23) : 0.0f};
+}
+__device__ __forceinline__ uint32_t e2m1_group(uint32_t top, const E2m1Row& row) {
+    // (rows without codes: 0; a row that is not finite must not bring its infinity in)
+    const float want = row.to == 0.0f ? 0.0f : __fmul_rn(__fmul_rn(__uint_as_float(top), row.to), 1.0f / 6.0f);
+    uint16_t two;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.0f), "f"(want));
+    return two;
+}
+__device__ __forceinline__ uint32_t e2m1_codes(const float (&x)[8], uint32_t byte, const E2m1Row& row) {
+    if (byte == 0) return 0;
+    const uint32_t wide = e4m3x2_to_f16x2(byte);
+    const float g = __low2float(*reinterpret_cast<const __half2*>(&wide)), inv = __frcp_rn(g);
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {                             // the correctly rounded quotient, as for the 8-bit codes
+        const float xs = __fmul_rn(x[e], row.to), q = __fmul_rn(xs, inv);
+        y[e] = __fmaf_rn(__fmaf_rn(-q, g, xs), inv, q);
+    }
+    uint32_t codes;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(codes) : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+    return codes;
+}
+
 // A lane's eight values of one head's row (the kDim / 8 lanes of the row call together) into codes and scale.  top: the lane's largest
 // magnitude, as bits: a NaN's pattern is above an infinity's, so either makes the scale NaN.
 template <int kFmt, int kDim>
@@ -150,35 +187,11 @@ __device__ __forceinline__ void kv_store_codes(const KvView& cache, int which, c
         top = pair;
 #pragma unroll
         for (int d = kLanes / 2; d > 1; d >>= 1) top = max(top, __shfl_xor_sync(group, top, d));
-        const bool finite = top < 0x7f800000u;
-        // the least power of two of which 6 * 448 = 1.3125 * 2^11 times is not below the largest magnitude
-        const int k = max(int(top >> 23) - 138 + ((top & 0x7fffffu) > 0x280000u ? 1 : 0), -126);
-        const float s = finite ? (top == 0 ? 0.0f : __uint_as_float(uint32_t(k + 127) << 23)) : __uint_as_float(0x7fc00000u);
-        uint32_t codes = 0, byte = 0;
-        if (finite && top != 0) {
-            const float to = __uint_as_float(uint32_t(127 - k) << 23);        // 1 / s
-            uint16_t two;
-            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.0f), "f"(__fmul_rn(__fmul_rn(__uint_as_float(pair), to), 1.0f / 6.0f)));
-            byte = two;
-            if (byte != 0) {
-                const uint32_t wide = e4m3x2_to_f16x2(byte);
-                const float g = __low2float(*reinterpret_cast<const __half2*>(&wide)), inv = __frcp_rn(g);
-                float y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {                                  // the correctly rounded quotient, as below
-                    const float xs = __fmul_rn(x[e], to), q = __fmul_rn(xs, inv);
-                    y[e] = __fmaf_rn(__fmaf_rn(-q, g, xs), inv, q);
-                }
-                asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-                    "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
-                    "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
-                    "mov.b32 %0, {a, b, c, d};\n\t}"
-                    : "=r"(codes) : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
-            }
-        }
+        const E2m1Row row = e2m1_row(top);
+        const uint32_t byte = e2m1_group(pair, row), codes = e2m1_codes(x, byte, row);
         *reinterpret_cast<uint32_t*>(dst + l * 4) = codes;
         if ((l & 1) == 0) cache.group[which][at.group_at + int64_t(head) * cache.group_head_stride + (l >> 1)] = char(byte);
-        if (l == 0) cache.scale[which][at.scale_at + int64_t(head) * cache.scale_head_stride] = s;
+        if (l == 0) cache.scale[which][at.scale_at + int64_t(head) * cache.scale_head_stride] = row.scale;
     } else {
 #pragma unroll
         for (int d = kLanes / 2; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(group, top, d));
