@@ -30,7 +30,7 @@ struct FourShape {
     static constexpr int kWarps = 4, kThreads = kWarps * 32, kTile = kWarps * 16;
     static constexpr int kAcc = kDim / 4 * kNT;                    // accumulators of a thread
     static constexpr bool kQRegs = kDim / 8 * kNT <= 32;           // queries of a thread fit its registers
-    static constexpr int kCtasPerSm = kAcc <= 32 ? 4 : kAcc <= 64 ? 3 : 2;
+    static constexpr int kCtasPerSm = kAcc <= 32 ? 4 : 2;
     static constexpr int kSub = kAcc <= 64 && kDim <= 128 ? 2 : 1;                // sub-tiles of 16 tokens a warp takes at a time
     static constexpr int kKBytes = kRowBytes / 4 < 16 ? kRowBytes / 4 : 16, kKChunks = kRowBytes / 4 / kKBytes, kKPiece = 2 * kKBytes;
     static constexpr int kVBytes = kRowBytes / 8, kVPiece = 2 * kVBytes;
@@ -64,6 +64,8 @@ template <int kDim>
 __device__ __forceinline__ int four_value_swap(int row) { return kDim == 256 ? (row & 3) * 2 : kDim == 128 ? (row >> 1 & 1) * 2 : 0; }
 template <int kDim>
 __device__ __forceinline__ int four_key_swap(int token) { return kDim == 256 ? (token & 1) * 4 : 0; }
+
+constexpr float kFourNoMax = -3.0e38f;   // in place of a maximum while a row has seen nothing
 
 template <int kDim, int kNT>
 __global__ void __launch_bounds__(FourShape<kDim, kNT>::kThreads, FourShape<kDim, kNT>::kCtasPerSm)
@@ -129,6 +131,7 @@ attend_four_kernel(const AttendParams p) {
         int pages = load_page(lane), pages_next = load_page(lane + 32);
         pages = checked(pages, lane);
         uint32_t bad_any = 0;
+        uint32_t fill_at = 0, use_at = 0;                                // offsets of the next stage to fill and to use
         auto issue = [&](int i) {                                        // starts the copies of sub-tile i (whole warp, i upwards)
             if (i < count) {
                 if (i > 0 && (i & 31) == 0) {
@@ -141,7 +144,8 @@ attend_four_kernel(const AttendParams p) {
                 bad_any |= ok ? 0u : 1u;
                 const int line = (pos_first + i * S::kTile) & pos_mask;
                 const int64_t at = int64_t(page) * p.cache.page_stride + int64_t(uint32_t(line)) * ts;
-                const uint32_t dst = ring + uint32_t((i % S::kStages) * S::kStageBytes);
+                const uint32_t dst = ring + fill_at;
+                fill_at = fill_at == (S::kStages - 1) * S::kStageBytes ? 0 : fill_at + S::kStageBytes;
 #pragma unroll
                 for (int r = 0; r < kCopies; ++r) {
                     const int tok = lane / kChunks + r * kPerCopy, c = lane % kChunks, row = four_value_row<kDim>(tok);
@@ -222,7 +226,7 @@ attend_four_kernel(const AttendParams p) {
             for (int j = 0; j < S::kTiles; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[nt][j][e] = 0.0f;
-            m[nt][0] = m[nt][1] = -INFINITY;
+            m[nt][0] = m[nt][1] = kFourNoMax;
             l[nt][0] = l[nt][1] = 0.0f;
         }
         const int tiles_n = (rows + 7) / 8;                              // of 8 rows
@@ -239,7 +243,8 @@ attend_four_kernel(const AttendParams p) {
 #pragma unroll
             for (int u = 0; u < S::kSub; ++u) {
                 here[u] = u == 0 || i + u < count;
-                st[u] = ring_gen + ((i + u) % S::kStages) * S::kStageBytes;
+                st[u] = ring_gen + use_at;
+                use_at = use_at == (S::kStages - 1) * S::kStageBytes ? 0 : use_at + S::kStageBytes;
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
@@ -289,9 +294,9 @@ attend_four_kernel(const AttendParams p) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float ks = sc[g + 8 * h], vs = sc[16 + g + 8 * h] * kGroupUnit;
-                    // A row of zero values has scale 0: the floor in its place gives it its share of the sum.  A NaN
+                    // A row of zero values has scale 0: the floor in its place (and in a NaN's) gives it its share of the sum.  A NaN
                     // scale reaches the score alone (the product with 0), which a mask can still replace.
-                    const float v = vs >= kScaleFloor ? vs : kScaleFloor;
+                    const float v = fmaxf(vs, kScaleFloor);
                     const float lv = fmaf(vs, 0.0f, lg2(v));
                     rvs[u][h] = __fdividef(1.0f, v);
 #pragma unroll
@@ -359,11 +364,9 @@ attend_four_kernel(const AttendParams p) {
                 uint32_t b[kNT][2];
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
-                    // (a row that has seen nothing yet has maximum -inf: any finite number serves in its place)
-                    const float m0 = m[nt][0] == -INFINITY ? 0.0f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.0f : m[nt][1];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const float e0 = ex2(s[u][nt][2 * h] - m0), e1 = ex2(s[u][nt][2 * h + 1] - m1);
+                        const float e0 = ex2(s[u][nt][2 * h] - m[nt][0]), e1 = ex2(s[u][nt][2 * h + 1] - m[nt][1]);
                         l[nt][0] = fmaf(e0, rvs[u][h], l[nt][0]);
                         l[nt][1] = fmaf(e1, rvs[u][h], l[nt][1]);
                         b[nt][h] = transpose_8x8(pack_f16(e0, e1));
