@@ -43,7 +43,7 @@ constexpr int kRopeThreads = 256;
 // (pairs v * 8 .. + 7: one vector from each half of the turned part, or two neighbouring ones), or one vector of the elements that
 // stay.  The items of a head lie on neighbouring lanes, so a lane works out its eight angles once for all the heads it sees.
 template <bool kF32>
-__global__ void __launch_bounds__(kRopeThreads) rope_rows_kernel(const RopeRowsParams p) {
+__global__ void __launch_bounds__(kRopeThreads, kF32 ? 3 : 4) rope_rows_kernel(const RopeRowsParams p) {
     pdl_wait();
     pdl_launch_dependents();
     constexpr int kItem = kF32 ? 4 : 2;
@@ -70,12 +70,23 @@ __global__ void __launch_bounds__(kRopeThreads) rope_rows_kernel(const RopeRowsP
             }
             const int a_at = (p.rope.interleaved ? item * 16 : item * 8) * kItem;
             const int b_at = (p.rope.interleaved ? item * 16 + 8 : p.rope.rot / 2 + item * 8) * kItem;
-#pragma unroll 2
-            for (int h = h0 + lane / lanes; h < h1; h += side) {
+            // (the next head's vectors are asked for before this one's are used)
+            struct Raw { uint4 v[kF32 ? 2 : 1]; } a_raw, b_raw, a_next = {}, b_next = {};
+            auto fetch = [&](int h) {
+                if (h >= h1) return;
+                const char* const src = x_row + int64_t(h) * p.dim * kItem;
+                a_next = *reinterpret_cast<const Raw*>(src + a_at);
+                b_next = *reinterpret_cast<const Raw*>(src + b_at);
+            };
+            int h = h0 + lane / lanes;
+            fetch(h);
+            for (; h < h1; h += side) {
+                a_raw = a_next, b_raw = b_next;
+                fetch(h + side);
                 float a[8], b[8], u[8], v[8];
                 const int64_t at = int64_t(h) * p.dim * kItem;
-                load8(x_row + at + a_at, kF32, a);
-                load8(x_row + at + b_at, kF32, b);
+                load8(reinterpret_cast<const char*>(&a_raw), kF32, a);
+                load8(reinterpret_cast<const char*>(&b_raw), kF32, b);
                 if (p.rope.interleaved) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
