@@ -62,15 +62,9 @@ __global__ void __launch_bounds__(kRopeThreads, kF32 ? 3 : 4) rope_rows_kernel(c
     char* const out_row = p.out + token * p.out_stride;
     for (int item = lane % lanes; item < items; item += lanes) {
         if (item < pair_items) {
-            float c[8], s[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                rope_angle(__ldg(p.rope.turns + item * 8 + e), position, p.rope.amplitude, &c[e], &s[e]);
-                if (p.inverse) s[e] = -s[e];
-            }
             const int a_at = (p.rope.interleaved ? item * 16 : item * 8) * kItem;
             const int b_at = (p.rope.interleaved ? item * 16 + 8 : p.rope.rot / 2 + item * 8) * kItem;
-            // (the next head's vectors are asked for before this one's are used)
+            // (a head's vectors are asked for ahead of the angles, or of the use of the last head's)
             struct Raw { uint4 v[kF32 ? 2 : 1]; } a_raw, b_raw, a_next = {}, b_next = {};
             auto fetch = [&](int h) {
                 if (h >= h1) return;
@@ -80,6 +74,12 @@ __global__ void __launch_bounds__(kRopeThreads, kF32 ? 3 : 4) rope_rows_kernel(c
             };
             int h = h0 + lane / lanes;
             fetch(h);
+            float c[8], s[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                rope_angle(__ldg(p.rope.turns + item * 8 + e), position, p.rope.amplitude, &c[e], &s[e]);
+                if (p.inverse) s[e] = -s[e];
+            }
             for (; h < h1; h += side) {
                 a_raw = a_next, b_raw = b_next;
                 fetch(h + side);
@@ -169,13 +169,11 @@ struct RopeAppendParams {
 // reads again).  The angles are the lane's for every head.
 struct RopeLane {
     float c[8], s[8];                    // s with the sign that the partner's term has; elements that stay: 1 and 0
-    int partner;                         // element the partner vector starts at (TL_ROPE_HALF, aligned), or -1: by elements
     bool turned;
 };
 __device__ __forceinline__ void rope_lane(const RopeView& r, int d0, int position, RopeLane* out) {
     const int half = r.rot / 2;
     out->turned = d0 < r.rot;
-    out->partner = -1;
 #pragma unroll
     for (int e = 0; e < 8; ++e) out->c[e] = 1.0f, out->s[e] = 0.0f;
     if (!out->turned) return;
@@ -199,22 +197,21 @@ __device__ __forceinline__ void rope_lane(const RopeView& r, int d0, int positio
         out->c[e] = c;
         out->s[e] = d < half ? -s : s;
     }
-    if (half % 8 == 0) out->partner = d0 < half ? d0 + half : d0 - half;
 }
 // The partners of elements d0 .. d0 + 7 of the head's row at `row`.
 template <bool kF32>
-__device__ __forceinline__ void rope_partners(const RopeView& r, const RopeLane& lane, const char* row, int d0, const float (&x)[8], float (&y)[8]) {
+__device__ __forceinline__ void rope_partners(const RopeView& r, const char* row, int d0, const float (&x)[8], float (&y)[8]) {
     if (r.interleaved) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
         return;
     }
     constexpr int kItem = kF32 ? 4 : 2;
-    if (lane.partner >= 0) {
-        load8(row + lane.partner * kItem, kF32, y);
+    const int half = r.rot / 2;
+    if (half % 8 == 0) {
+        load8(row + (d0 < half ? d0 + half : d0 - half) * kItem, kF32, y);
         return;
     }
-    const int half = r.rot / 2;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int d = d0 + e;
@@ -227,7 +224,7 @@ __device__ __forceinline__ void rope_partners(const RopeView& r, const RopeLane&
 
 // A warp takes one row's heads, kCopyAhead groups of them: of the queries, of the keys or of the values (blockIdx.y).
 template <int kFmt, int kDim, bool kF32>
-__global__ void __launch_bounds__(kCopyThreads) rope_append_kernel(const RopeAppendParams p) {
+__global__ void __launch_bounds__(kCopyThreads, 2) rope_append_kernel(const RopeAppendParams p) {
     pdl_wait();
     pdl_launch_dependents();
     constexpr int kLanes = kDim / 8, kPerWarp = 32 / kLanes, kItem = kF32 ? 4 : 2;
@@ -244,17 +241,18 @@ __global__ void __launch_bounds__(kCopyThreads) rope_append_kernel(const RopeApp
 #pragma unroll
         for (int i = 0; i < kCopyAhead; ++i)
             if (head0 + i * kPerWarp < heads) load8(src + (int64_t(head0 + i * kPerWarp) * kDim + l * 8) * kItem, kF32, x[i]);
+        // (partners too, ahead of everything that is looked up)
+        float y[kCopyAhead][8];
+#pragma unroll
+        for (int i = 0; i < kCopyAhead; ++i)
+            if (which != 1 && l * 8 < p.rope.rot && head0 + i * kPerWarp < heads)
+                rope_partners<kF32>(p.rope, src + int64_t(head0 + i * kPerWarp) * kDim * kItem, l * 8, x[i], y[i]);
         KvRowPlace at;
         at.pos = 0;
         const bool owned = kv_locate_row(p.cache, p.batch, row, kDim / 16, &at);
         if (which != 1) {
             RopeLane turn;
             rope_lane(p.rope, l * 8, p.positions ? p.positions[row] : owned ? at.pos : 0, &turn);
-            float y[kCopyAhead][8];
-#pragma unroll
-            for (int i = 0; i < kCopyAhead; ++i)
-                if (turn.turned && head0 + i * kPerWarp < heads)
-                    rope_partners<kF32>(p.rope, turn, src + int64_t(head0 + i * kPerWarp) * kDim * kItem, l * 8, x[i], y[i]);
             __syncwarp();                                     // (queries may be turned in place: every lane has what it needs)
             if (turn.turned) {
 #pragma unroll
