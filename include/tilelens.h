@@ -29,7 +29,7 @@
  *     current device; the internal split-K workspace belongs to the device, so calls that can run at the same
  *     time on one GPU (two streams, two threads) must each bring their own workspace.
  *   - Stream capture.  Every call that only enqueues work (the relayouts, the device-buffer products, tl_moe_ffn,
- *     tl_read_amp_async / tl_read_amp_batch, tl_hw_*) may be issued on a stream that is being captured into a CUDA
+ *     tl_kv_*, tl_tree_*, tl_rope_rows / tl_rope_append, tl_page_*, tl_read_amp_async / tl_read_amp_batch, tl_hw_*) may be issued on a stream that is being captured into a CUDA
  *     graph, and the graph replays the same launches with the same bits: nothing a launch needs lives in host state
  *     that a replay would miss.  Two conditions.  The library's first use of a device, a kernel or a problem shape
  *     allocates and configures (control block, shared-memory attributes, tensor maps), which a capture forbids: make
@@ -660,7 +660,7 @@ int tl_rope_rows(const tl_rope* rope, const void* d_x, int64_t x_stride, void* d
  *   d_q          [tokens][q_heads][head_dim] of type elem, or NULL with q_heads 0.  d_q_out may be d_q if elem is bf16.
  *   d_k, d_v     as in tl_kv_append.  Pointers and strides are multiples of 16 bytes.
  * Queries of a row that no request owns, or that has no page, are turned all the same (by position 0 with d_positions NULL where no
- * request owns it).  Asynchronous.
+ * request owns it); a batch without requests does nothing.  Asynchronous.
  */
 int tl_rope_append(const tl_kv_cache* cache, const tl_kv_batch* batch, const tl_rope* rope, const int32_t* d_positions, const void* d_q,
                    int64_t q_stride, int q_heads, void* d_q_out, int64_t q_out_stride, const void* d_k, const void* d_v, int elem,
@@ -697,7 +697,8 @@ typedef struct tl_page_tables {
  * order of requests, *d_n_moves how many; entries behind those are left alone.
  * If the free pages do not suffice nothing changes, *d_n_moves is 0 and *d_missing says how many more it takes; else it is 0.
  * Positions past the table are left out and reported (tl_device_status, detail 0xa00).
- * Scratch comes from the workspace (tl_page_workspace_bytes).  Asynchronous.
+ * Scratch comes from the workspace (tl_page_workspace_bytes; like that of forking and compacting, and of a captured call from
+ * tl_set_workspace alone).  Asynchronous.
  */
 int tl_page_reserve(const tl_page_tables* tables, const int32_t* d_start, const int32_t* d_tokens, int32_t* d_moves, int32_t* d_n_moves,
                     int32_t* d_missing, void* cuda_stream);

@@ -138,14 +138,15 @@ def test_compacting(most):
 
 
 @pytest.mark.parametrize("requests,width,pages,page,seed", [(1, 1, 1, 16, 0), (3, 4, 7, 16, 1), (17, 20, 200, 32, 2), (64, 12, 500, 16, 3),
-                                                            (300, 9, 2500, 64, 4), (1500, 6, 9001, 16, 5), (40, 300, 40007, 16, 6)])
+                                                            (300, 9, 2500, 64, 4), (1500, 6, 9001, 16, 5), (40, 300, 40007, 16, 6),
+                                                            (60, 300, 140003, 16, 7), (9000, 2, 131073, 16, 8)])
 def test_long_traffic(requests, width, pages, page, seed):
     """Random reservations, forks, releases and compactions, the tables compared after each."""
     rng = random.Random(seed)
     b = Both(requests, width, pages, page)
     length = [0] * requests
     room = width * page
-    for turn in range(30 if requests < 100 else 10):
+    for turn in range(30 if pages < 10 ** 5 and requests < 100 else 10):
         kind = rng.choice(["grow", "grow", "back", "fork", "release", "compact"])
         if kind in ("grow", "back"):
             start, tokens = [], []
@@ -172,6 +173,20 @@ def test_long_traffic(requests, width, pages, page, seed):
             length = [n if k < 0 else min(n, k) for n, k in zip(length, keep)]
         else:
             b.compact(rng.choice([None, 2]) if pages > 2 else None)
+    b.tl.device_status()
+
+
+@pytest.mark.parametrize("pages", [2 ** 17, 2 ** 17 + 1, 300000])
+def test_the_last_pages_of_a_large_pool(pages):
+    """One CTA up to 2^17 pages, a cluster beyond: all but the last few pages are held, forks write, and everything moves to the front."""
+    b = Both(6, pages, pages)
+    room = (pages - 20) * 16
+    b.reserve([0] * 6, [room, 30, -1, -1, -1, -1])
+    b.fork([1, 1, 0], [2, 3, 4], [30, 20, 35])
+    assert b.reserve([-1, 30, 30, 20, 35, -1], [-1, 40, 40, 40, 40, 400]) > 0
+    assert b.reserve([-1, 30, 30, 20, 35, -1], [-1, 40, 40, 40, 40, 90]) == 0
+    b.release([100, -1, -1, 0, -1, -1])
+    b.compact()
     b.tl.device_status()
 
 
