@@ -20,9 +20,12 @@ struct PageView {
 };
 
 constexpr int kPageThreads = 1024, kPageWarps = kPageThreads / 32;
-// CTAs that look through a pool: one, whose barriers cost next to nothing, up to 2^17 pages, else a cluster of eight (the barrier of a
-// cluster that orders global memory took about a microsecond, and there are five of them).
-constexpr int kPageCtas = 8, kPagesOfOne = 1 << 17;
+// CTAs that look through a pool: one, whose barriers cost little, or (larger pools) a cluster of eight.  us per call, one CTA / cluster, 512
+// requests, calls back to back:
+//   reserve (nothing to take)     32768 pages 6.1 (the host's call) / 11.7, 65536 8.6 / 11.6, 131072 14.2 / 11.8, 2^20 92 / 18.6
+//   compact (nothing to move)     16384 pages 11.5 / 14.2, 32768 13.0 / 14.9, 65536 28 / 16.3, 131072 57 / 16.7, 2^20 469 / 73
+// One turn of one CTA is 32768 pages; compacting touches every page of a turn, reserving only as many as it takes.
+constexpr int kPageCtas = 8, kReserveOfOne = 1 << 16, kCompactOfOne = 1 << 15;
 
 // What a reserving call keeps per page it may take from somebody (written before it is read).
 struct PageClaim {
@@ -603,11 +606,11 @@ static size_t page_workspace(const PageView& t, int forks) {
     return std::max(std::max(reserve, compact), up16(size_t(forks) * 4));
 }
 
-// A kernel that looks through the pool: one CTA, or a cluster.
+// A kernel that looks through the pool: one CTA up to `of_one` pages, or a cluster.
 template <typename P>
-static int page_launch(const PageView& t, void (*one)(P), void (*cluster)(P), const P& p, cudaStream_t stream) {
+static int page_launch(const PageView& t, int of_one, void (*one)(P), void (*cluster)(P), const P& p, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    const bool single = t.pages <= kPagesOfOne;
+    const bool single = t.pages <= of_one;
     cfg.gridDim = dim3(single ? 1 : kPageCtas);
     cfg.blockDim = dim3(kPageThreads);
     cfg.stream = stream;
@@ -664,7 +667,7 @@ int tl_page_reserve(const tl_page_tables* tables, const int32_t* d_start, const 
     p.n_moves = d_n_moves;
     p.missing = d_missing;
     p.status = dev().ctl.d_status;
-    return page_launch(p.t, page_reserve_kernel<1>, page_reserve_kernel<kPageCtas>, p, stream);
+    return page_launch(p.t, kReserveOfOne, page_reserve_kernel<1>, page_reserve_kernel<kPageCtas>, p, stream);
 }
 
 int tl_page_release(const tl_page_tables* tables, const int32_t* d_tokens, void* cuda_stream) {
@@ -724,7 +727,7 @@ int tl_page_compact(const tl_page_tables* tables, int32_t* d_moves, int most, in
     p.in_use = d_in_use;
     p.most = most;
     p.status = dev().ctl.d_status;
-    if (int rc = page_launch(p.t, page_compact_kernel<1>, page_compact_kernel<kPageCtas>, p, stream)) return rc;
+    if (int rc = page_launch(p.t, kCompactOfOne, page_compact_kernel<1>, page_compact_kernel<kPageCtas>, p, stream)) return rc;
     if (p.t.requests == 0) return TL_OK;
     return kv_launch(page_rename_kernel, dim3(unsigned(ceil_div(p.t.requests, 8))), 256, stream, p.t, const_cast<const int32_t*>(p.went),
                      const_cast<const int32_t*>(p.sums), p.status);

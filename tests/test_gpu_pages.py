@@ -176,9 +176,9 @@ def test_long_traffic(requests, width, pages, page, seed):
     b.tl.device_status()
 
 
-@pytest.mark.parametrize("pages", [2 ** 17, 2 ** 17 + 1, 300000])
+@pytest.mark.parametrize("pages", [2 ** 15, 2 ** 15 + 1, 2 ** 16, 2 ** 16 + 1, 2 ** 17, 2 ** 17 + 1, 300000])
 def test_the_last_pages_of_a_large_pool(pages):
-    """One CTA up to 2^17 pages, a cluster beyond: all but the last few pages are held, forks write, and everything moves to the front."""
+    """One CTA up to 2^15 (compacting) or 2^16 pages, a cluster beyond: all but the last few pages are held, forks write, and everything moves to the front."""
     b = Both(6, pages, pages)
     room = (pages - 20) * 16
     b.reserve([0] * 6, [room, 30, -1, -1, -1, -1])
