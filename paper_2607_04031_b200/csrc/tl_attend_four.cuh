@@ -10,7 +10,7 @@
 // unused (a 16-row query operand leaves half): 16 products, 4 scores per thread and 32 accumulators for 16 tokens of 128 dimensions.
 // Thread (g = lane / 4, t = lane % 4) holds
 //   K      tokens g, g + 8; the contraction index may be permuted as long as q is, so its share is a contiguous piece of the row;
-//   q^T    row g, the same piece, in registers for the whole unit (in shared memory where those do not suffice);
+//   q^T    row g, the same piece, in shared memory for the whole unit;
 //   S^T    tokens g, g + 8 of rows 2t, 2t + 1.  P^T as the second product wants it (row g, tokens 2t, 2t + 1) is that transposed
 //          8 x 8 by 8 x 8, one movmatrix each;
 //   V^T    tokens 2t, 2t + 1, 2t + 8, 2t + 9 of a contiguous piece of dimensions; the codes of two tokens at one dimension are put
@@ -29,15 +29,14 @@ struct FourShape {
     static constexpr int kRowBytes = kDim / 2, kGroups = kDim / 16, kRows = kNT * 8;
     static constexpr int kWarps = 4, kThreads = kWarps * 32, kTile = kWarps * 16;
     static constexpr int kAcc = kDim / 4 * kNT;                    // accumulators of a thread
-    static constexpr bool kQRegs = kDim / 8 * kNT <= 32;           // queries of a thread fit its registers
     static constexpr int kCtasPerSm = kAcc <= 32 ? 4 : 2;
-    static constexpr int kSub = kAcc <= 64 && kDim <= 128 ? 2 : 1;                // sub-tiles of 16 tokens a warp takes at a time
+    static constexpr int kSub = kAcc <= 32 && kDim <= 128 ? 2 : 1;                // sub-tiles of 16 tokens a warp takes at a time
     static constexpr int kKBytes = kRowBytes / 4 < 16 ? kRowBytes / 4 : 16, kKChunks = kRowBytes / 4 / kKBytes, kKPiece = 2 * kKBytes;
     static constexpr int kVBytes = kRowBytes / 8, kVPiece = 2 * kVBytes;
     static constexpr int kSteps = kDim / 16, kTiles = kDim / 16;   // 16-deep steps of K q^T, 16-row tiles of V^T P^T
     static constexpr int kValueAt = 16 * kRowBytes, kScaleAt = 32 * kRowBytes, kGroupAt = kScaleAt + 128;
     static constexpr int kStageBytes = kGroupAt + 32 * kGroups;
-    static constexpr int kQBytes = kQRegs ? 0 : kNT * kSteps * 256;
+    static constexpr int kQBytes = kNT * kSteps * 256;
     static constexpr int kStatBytes = (kWarps * kRows * 2 + kRows * 3) * 4;
     static constexpr int kBudget = 225 * 1024 / kCtasPerSm - 1024 - kQBytes - kStatBytes;
     static constexpr int kStagesFit = kBudget / (kWarps * kStageBytes);
@@ -164,12 +163,10 @@ attend_four_kernel(const AttendParams p) {
 #pragma unroll
         for (int i = 0; i < S::kStages - S::kSub; ++i) issue(i);
 
-        // The queries: thread (g, t) takes its piece of row nt * 8 + g, scaled to f16 by a power of two of the row's own.
-        uint32_t q[S::kQRegs ? kNT : 1][S::kSteps][2];
-        float fac[kNT][2];
+        // The queries, a block of 8 rows per warp: thread (g, t) takes its piece of row nt * 8 + g, scaled to f16 by a power of two of the row's own.
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt) {
-            if (!S::kQRegs && nt % S::kWarps != warp) continue;
+            if (nt % S::kWarps != warp) continue;
             const int r = nt * 8 + g, row = w.block * S::kRows + r;
             uint32_t u[S::kSteps][2];
             if (r < rows) {
@@ -200,22 +197,14 @@ attend_four_kernel(const AttendParams p) {
             for (int i = 0; i < S::kSteps; ++i)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) u[i][k] = pack_f16(__uint_as_float(u[i][k] << 16) * mul, __uint_as_float(u[i][k] & 0xffff0000u) * mul);
-            if constexpr (S::kQRegs) {
 #pragma unroll
-                for (int i = 0; i < S::kSteps; ++i) q[nt][i][0] = u[i][0], q[nt][i][1] = u[i][1];
-                fac[nt][0] = __shfl_sync(0xffffffffu, f, 8 * t);
-                fac[nt][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
-            } else {
-#pragma unroll
-                for (int i = 0; i < S::kSteps; ++i) q_frag[(nt * S::kSteps + i) * 32 + lane] = make_uint2(u[i][0], u[i][1]);
-                if (t == 0) row_fac[r] = f;
-            }
+            for (int i = 0; i < S::kSteps; ++i) q_frag[(nt * S::kSteps + i) * 32 + lane] = make_uint2(u[i][0], u[i][1]);
+            if (t == 0) row_fac[r] = f;
         }
-        if (!S::kQRegs) {
-            __syncthreads();
+        __syncthreads();
+        float fac[kNT][2];
 #pragma unroll
-            for (int nt = 0; nt < kNT; ++nt) fac[nt][0] = row_fac[nt * 8 + 2 * t], fac[nt][1] = row_fac[nt * 8 + 2 * t + 1];
-        }
+        for (int nt = 0; nt < kNT; ++nt) fac[nt][0] = row_fac[nt * 8 + 2 * t], fac[nt][1] = row_fac[nt * 8 + 2 * t + 1];
 
         // o[nt][j]: dimensions 2j, 2j + 1 of the thread's piece ([0], [2]) of row nt * 8 + 2t, and ([1], [3]) of row + 1
         float o[kNT][S::kTiles][4];
@@ -275,12 +264,8 @@ attend_four_kernel(const AttendParams p) {
 #pragma unroll
                             for (int nt = 0; nt < kNT; ++nt) {
                                 if (kNT > 2 && nt >= tiles_n) continue;
-                                if constexpr (S::kQRegs) {
-                                    mma_16816<false>(s[u][nt], a, q[nt][step][0], q[nt][step][1]);
-                                } else {
-                                    const uint2 b = q_frag[(nt * S::kSteps + step) * 32 + lane];
-                                    mma_16816<false>(s[u][nt], a, b.x, b.y);
-                                }
+                                const uint2 b = q_frag[(nt * S::kSteps + step) * 32 + lane];
+                                mma_16816<false>(s[u][nt], a, b.x, b.y);
                             }
                         }
                     }
