@@ -107,6 +107,11 @@ static auto attend_tc_of(int format) {
 //                                                    32 rows: 16 requests bf16 87 / 87, E4M3 77 / 71, 64 requests INT8 144 / 130
 //                                    head_dim 64     32 rows: 16 requests bf16 60 / 69, E4M3 48 / 60; one request equal
 //                                    (either)        64 rows: 16 requests bf16 146 / 93, E4M3 126 / 77
+//     over 4 bits                    head_dim 128    32 rows: 1 request 25 / 24, 16 requests 57 / 74, 64 requests 99 / 135
+//                                                    40 rows (blocks of 32): 1 request 23 / 24, 4 requests 36.4 / 34.8, 16 89 / 74, 64 165 / 136
+//                                    head_dim 64     32 rows: 1 request 19.5 / 21, 16 requests 42 / 65; 48 rows: 1 request 19 / 21,
+//                                                    4 requests 28 / 30, 16 63 / 65, 64 118 / 119; 64 rows: 4 29 / 31, 64 122 / 120;
+//                                                    4 requests of 39 over 1531, 9 heads 19.2 / 18.9
 //   blocks of 128 or 256 rows, us:   256 rows, contexts of half the length to all of it:
 //                                    1 request over 4100 (1.8 tiles of 256 rows per SM) bf16 34 / 44, E4M3 36 / 42
 //                                    4 over 8000 (10.8) bf16 76 / 79, E4M3 73 / 76; 8 over 2000 (5.6) 65 / 68, 55 / 60
@@ -123,7 +128,8 @@ static int attend_plan(const tl_kv_cache* cache, const tl_kv_batch* batch, int q
     const int64_t room = std::min(batch->table_stride * cache->page_tokens, kKvMaxTokens);
     int64_t sms = dev().sm_count;
     if (opt(TL_OPT_SM_LIMIT) > 0) sms = std::min(sms, opt(TL_OPT_SM_LIMIT));
-    if (cache->head_dim <= 128 && rows > (cache->head_dim == 128 && cache->format != TL_KV_E2M1 ? 24 : 32)) {
+    const int64_t few = cache->format == TL_KV_E2M1 ? (cache->head_dim == 64 ? 48 : 32) : cache->head_dim == 128 ? 24 : 32;
+    if (cache->head_dim <= 128 && rows > few) {
         plan->tile_tokens = 128;
         plan->ctas_per_sm = 1;
         const double positions = std::min(double(batch->requests) * double(room), double(cache->pages) * cache->page_tokens);

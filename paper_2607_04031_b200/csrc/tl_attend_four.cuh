@@ -18,6 +18,16 @@
 // Codes become f16 by one conversion per pair, times their group scales (kGroupUnit): exact.  Scales, weights, references and what
 // masked positions may hold: as over an 8-bit cache; no code or group scale reads as infinite or NaN, so positions past the end need
 // no zeros in their place.
+//
+// Measured choices.  Queries in registers took as long with one block of 8 rows and 2 to 12 % longer with two and four.  Two sub-tiles a
+// turn: 32 requests of one token over 4100 (cold) 48 us, one a turn 54; beyond 32 accumulators one a turn took up to 13 % less with few
+// requests and 3 % more to 1 % less with 64.  CTAs per SM, the same call: four 46 to 48 us, three 50, five (too few registers) 56 to 58; with 64
+// accumulators three in place of two took 8 to 12 % less at 4 requests over 4100 and up to 7 % more elsewhere.
+//
+// What bounds it: 32 requests of one token over 4100 (64 query and 8 key/value heads of 128, 122 MB): 41 us, floor 18.6.  8.6 us pass
+// outside of the loop (launch, ranges, queries, joins); 20.8 million warp instructions keep the ALUs, which run unpacking and softmax at half
+// rate, busy for 49 % and the issue slots for 60 % of the time with four warps per scheduler; the copies alone (no arithmetic)
+// take 29.  Bulk copies in place of cp.async: as fast issued by each warp, 62 us by a warp of their own.
 #pragma once
 
 #include "tl_attend.cuh"

@@ -42,6 +42,9 @@ constexpr int kRopeThreads = 256;
 // A warp turns rows of one token.  An item is what a thread holds at once: two vectors of eight elements that are eight pairs
 // (pairs v * 8 .. + 7: one vector from each half of the turned part, or two neighbouring ones), or one vector of the elements that
 // stay.  The items of a head lie on neighbouring lanes, so a lane works out its eight angles once for all the heads it sees.
+// 8192 tokens x 72 heads x 128, bf16: 54 us for 302 MB (floor 46), HBM.  Angles through shared memory, worked out once per CTA, took
+// 76 to 111 us (60 here by the same clock, cold); polynomials in place of sincospi changed nothing: the angles are not what a warp waits for.  Small
+// calls are latency: 1501 tokens x 20 heads of 80 in fp32 8.2 us, floor 2.9.
 template <bool kF32>
 __global__ void __launch_bounds__(kRopeThreads, kF32 ? 3 : 4) rope_rows_kernel(const RopeRowsParams p) {
     pdl_wait();
@@ -223,6 +226,8 @@ __device__ __forceinline__ void rope_partners(const RopeView& r, const char* row
 }
 
 // A warp takes one row's heads, kCopyAhead groups of them: of the queries, of the keys or of the values (blockIdx.y).
+// A step of 32 tokens (64 query and 8 key/value heads of 128): 8 us, a chain of loads (the row's request, its page, positions, angles);
+// rows and partners are asked for ahead of it.
 template <int kFmt, int kDim, bool kF32>
 __global__ void __launch_bounds__(kCopyThreads, 2) rope_append_kernel(const RopeAppendParams p) {
     pdl_wait();
