@@ -25,8 +25,8 @@
 // accumulators three in place of two took 8 to 12 % less at 4 requests over 4100 and up to 7 % more elsewhere.
 //
 // What bounds it: 32 requests of one token over 4100 (64 query and 8 key/value heads of 128, 122 MB): 41 us, floor 18.6.  8.6 us pass
-// outside of the loop (launch, ranges, queries, joins); 20.8 million warp instructions keep the ALUs, which run unpacking and softmax at half
-// rate, busy for 49 % and the issue slots for 60 % of the time with four warps per scheduler; the copies alone (no arithmetic)
+// outside of the loop (launch, ranges, queries, joins); 20 million warp instructions keep the ALUs, which run unpacking and softmax at half
+// rate, busy for 48 % and the issue slots for 58 % of the time with four warps per scheduler; the copies alone (no arithmetic)
 // take 29.  Bulk copies in place of cp.async: as fast issued by each warp, 62 us by a warp of their own.
 #pragma once
 
