@@ -24,6 +24,14 @@ def test_matches_the_formula(dim, heads, group, counts):
     Step("e2m1", heads, group, dim, 32, ctx, counts, seed=dim + group).check()
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("heads,group,counts", [(2, 1, [8]), (2, 1, [9]), (1, 1, [17]), (1, 1, [24]), (2, 1, [32]), (2, 1, [33]), (1, 3, [13, 13, 13]),
+                                                (1, 1, [40]), (2, 1, [47]), (1, 8, [6, 6]), (2, 1, [49]), (1, 1, [70, 1, 1]), (2, 4, [30, 1, 0, 1, 1])])
+def test_rows_around_the_borders_of_blocks_and_kernels(dim, heads, group, counts):
+    """Blocks of 8, 16 and 32 rows, the last one full or not, requests of fewer and of more rows than their average."""
+    Step("e2m1", heads, group, dim, 32, [2900 if b == 0 else 131 * b for b in range(len(counts))], counts, trees="tree", seed=sum(counts)).check()
+
+
 @pytest.mark.parametrize("ctx", [0, 1, 15, 16, 17, 63, 64, 111, 127, 128, 129, 255, 257])
 @pytest.mark.parametrize("counts", [[1, 3], [40, 33]])
 def test_lengths_around_every_tile_border(ctx, counts):
