@@ -481,8 +481,8 @@ int tl_hw_box_load(const tl_hw_desc* desc, const void* d_src_tilemajor, uint64_t
  * TL_KV_E2M1 holds 4-bit codes (a sign, two bits of exponent, one of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6; element 2i in the low half
  * of byte i), one E4M3 byte per 16 elements and one fp32 scale per token and head: scale = the least power of two, 2^-126 at least,
  * with 6 * 448 * scale >= a; group scale = (max |x| of the 16) / scale * c, c = 1/6 in fp32, rounded to E4M3, ties to even;
- * code = x / (group scale * scale) rounded to the nearest, ties to even, 6 at most (0 under a group scale of 0).  The value held,
- * code * group scale * scale, has at most 6 bits: it is exact in bf16.  A row that is all zeros has scale and group scales 0, a row
+ * code = x / (group scale * scale) rounded to the nearest, ties to even, 6 at most, a zero with the sign of x (0 under a group scale
+ * of 0).  The value held, code * group scale * scale, has at most 6 bits: it is exact in bf16.  A row that is all zeros has scale and group scales 0, a row
  * with an infinity or a NaN has scale NaN.  Group scales in the memory of a page are read without their sign, 0x7f as 480, and row
  * scales have to be below 2^118.
  */

@@ -161,8 +161,9 @@ __device__ __forceinline__ uint32_t e2m1_codes(const float (&x)[8], uint32_t byt
     float y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {                             // the correctly rounded quotient, as for the 8-bit codes
+        // (With the remainder's sign the other way round a zero keeps its own: -0 * g + 0 = 0, then -0 * inv + -0 = -0.)
         const float xs = __fmul_rn(x[e], row.to), q = __fmul_rn(xs, inv);
-        y[e] = __fmaf_rn(__fmaf_rn(-q, g, xs), inv, q);
+        y[e] = __fmaf_rn(-__fmaf_rn(q, g, -xs), inv, q);
     }
     uint32_t codes;
     asm("{\n\t.reg .b8 a, b, c, d;\n\t"
