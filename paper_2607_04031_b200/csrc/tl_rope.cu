@@ -290,12 +290,13 @@ __global__ void __launch_bounds__(kCopyThreads, 2) rope_append_kernel(const Rope
 }
 
 // A row's depth: the steps from it to the root.  Parents lie strictly below, so the climb ends.
-__global__ void tree_positions_kernel(const int32_t* parents, const int32_t* offsets, const int32_t* start, int requests, int tokens,
+__global__ void __launch_bounds__(256) tree_positions_kernel(const int32_t* parents, const int32_t* offsets, const int32_t* start, int requests, int tokens,
                                       int32_t* positions) {
     pdl_wait();
     pdl_launch_dependents();
-    const int row = int(blockIdx.x * blockDim.x + threadIdx.x) / 32;
-    if (row >= tokens) return;
+    const int64_t at = int64_t(blockIdx.x) * 8 + threadIdx.x / 32;         // (a warp per row: threads pass 32 bits)
+    if (at >= tokens) return;
+    const int row = int(at);
     int b = -1, first = 0;
     for (int b0 = 0; b0 < requests && b < 0; b0 += 32) {
         const int mine = min(b0 + int(lane_id()), requests - 1);
