@@ -77,7 +77,8 @@ class Decoder:
         else:
             counts = lambda n: torch.zeros(n, dtype=torch.int32, device=device)  # noqa: E731
             self.page_table = torch.full((requests, pages), -1, dtype=torch.int32, device=device)
-            self.tables = tl.page_tables(self.page_table, counts(requests), counts(pool_pages), page_tokens)
+            self.held = counts(requests)
+            self.tables = tl.page_tables(self.page_table, self.held, counts(pool_pages), page_tokens)
             self.moves, self.n_moves, self.missing = torch.zeros(max(requests, pool_pages), 3, dtype=torch.int32, device=device), counts(1), counts(1)
         self.rope = None
         if rotary is not None:
@@ -139,11 +140,26 @@ class Decoder:
         if self.missing.item():
             raise RuntimeError(f"the pool has {self.missing.item()} pages too few")
 
-    def fork(self, samples: int):
-        """Request i * samples + j (j > 0) continues what request i * samples has so far, on the same pages until it writes them."""
+    def _continuations(self, samples: int) -> torch.Tensor:
+        """The requests that fork(samples) makes continuations of; raises where they cannot be."""
+        if samples < 1:
+            raise ValueError(f"samples: expected 1 or more, got {samples}")
         to = torch.tensor([r for r in range(self.requests) if r % samples], dtype=torch.int32, device=self.device)
+        if to.numel():
+            if self.tables is None:
+                raise ValueError("continuations share pages: the decoder needs a pool (pool_pages)")
+            if bool((self.held[to.long()] != 0).any()):
+                raise ValueError("a request that holds pages cannot become another's continuation")
+        return to
+
+    def fork(self, samples: int):
+        """Request i * samples + j (j > 0), which must hold nothing, continues what request i * samples has so far, on the same pages
+        until it writes them."""
+        to = self._continuations(samples)
         if to.numel() == 0:
             return
+        if self.last is None:
+            raise ValueError("nothing to continue: prefill comes first")
         from_ = to // samples * samples
         self.start[to.long()] = self.start[from_.long()]
         self.last[to.long()] = self.last[from_.long()]
@@ -151,6 +167,8 @@ class Decoder:
 
     def compact(self) -> int:
         """Moves the pages in use to the front of the pool and says how many they are."""
+        if self.tables is None:
+            raise ValueError("only a decoder with a pool (pool_pages) moves pages")
         tl.page_compact(self.tables, self.moves, self.n_moves, self.missing)
         tl.page_copy(self.cache, self.moves, self.n_moves)
         return int(self.missing.item())
@@ -217,6 +235,7 @@ class Decoder:
     def generate(self, prompts, new_tokens: int, branches: int = 3, depth: int = 4, samples: int = 1):
         """Lists of new token ids, `new_tokens` per request, and the number of passes that gave them.  samples: continuations of each
         prompt, neighbours among the requests (there are len(prompts) * samples)."""
+        self._continuations(samples)                         # (what stands against them is said before anything has changed)
         self.prefill([p if j == 0 else None for p in prompts for j in range(samples)])
         if samples > 1:
             self.fork(samples)
