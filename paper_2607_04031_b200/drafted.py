@@ -176,6 +176,8 @@ class Decoder:
     def prefill(self, prompts) -> Step | None:
         """prompts: one list of token ids per request, none empty (a request without one, None, is left for a fork).  All but their last
         tokens go through the layer."""
+        if len(prompts) != self.requests:
+            raise ValueError(f"expected {self.requests} prompts, one per request, got {len(prompts)}")
         self.last = torch.tensor([p[-1] if p else 0 for p in prompts], device=self.device)
         counts = [len(p) - 1 if p else 0 for p in prompts]
         prompts = [p or [0] for p in prompts]

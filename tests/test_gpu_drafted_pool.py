@@ -1,4 +1,4 @@
-"""What the decoding loop refuses about pools and forks, before anything has changed."""
+"""What the decoding loop refuses about pools, forks and prompts, before anything has changed."""
 import pytest
 import torch
 
@@ -64,4 +64,14 @@ def test_a_number_of_samples_that_is_none(samples):
     for call in (lambda: d.fork(samples), lambda: d.generate(PROMPTS, 4, 2, 2, samples=samples)):
         with pytest.raises(ValueError, match="samples"):
             call()
+    _unchanged(d, before)
+
+
+@pytest.mark.parametrize("prompts,samples", [([[5], [6]], 1), ([[5]], 2), ([[5, 6], [6, 7], [8, 9]], 2), ([[5], [6], [7], [8], [9]], 1), ([], 1), ([], 3)])
+def test_as_many_prompts_as_the_decoder_has_requests(prompts, samples):
+    # (prompts of one token go through no layer: nothing behind them would notice)
+    d = _decoder(pool_pages=40)
+    before = _state(d)
+    with pytest.raises(ValueError, match="prompts"):
+        d.generate(prompts, 4, 2, 2, samples=samples)
     _unchanged(d, before)
