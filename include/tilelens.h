@@ -689,12 +689,14 @@ typedef struct tl_page_tables {
 } tl_page_tables;
 
 /*
- * Gives requests pages that they may write: afterwards request b holds pages for d_tokens[b] positions (it keeps what it holds beyond
- * them), and those that hold the positions d_start[b] .. d_tokens[b] - 1 have no other holder.  A request with d_tokens[b] < 0 is left
+ * Gives requests pages that they may write: afterwards request b holds pages for d_tokens[b] positions (it keeps the pages that it holds
+ * beyond them), and those that hold the positions d_start[b] .. d_tokens[b] - 1 have no other holder.  A request with d_tokens[b] < 0 is left
  * alone.  Entries that are missing, and entries in that range that others hold too, get fresh pages: the lowest free ones, in the order
  * of requests and entries.  Where all holders of a page are to write it, the first of them (in that order) keeps it.  Of a replaced page
  * the rows in front of d_start[b] are to be copied: d_moves ([requests][3]: from, to, rows) receives what tl_page_copy is to do, in the
  * order of requests, *d_n_moves how many; entries behind those are left alone.
+ * Rows behind those are not carried over: a request that writes in the middle of what it holds, on shared pages, loses its positions from
+ * d_tokens[b] to the end of that page (a sequence that is taken back and written anew ends at d_tokens[b], and has none).
  * If the free pages do not suffice nothing changes, *d_n_moves is 0 and *d_missing says how many more it takes; else it is 0.
  * Positions past the table are left out and reported (tl_device_status, detail 0xa00).
  * Scratch comes from the workspace (tl_page_workspace_bytes; like that of forking and compacting, and of a captured call from

@@ -841,7 +841,7 @@ def page_reserve(tables: PageTables, start: torch.Tensor, tokens: torch.Tensor, 
                  missing: torch.Tensor, stream=None):
     """Pages for tokens[b] positions of every request (tokens[b] < 0: left alone), those of start[b] .. tokens[b] - 1 its own.  moves
     (int32 [requests or more, 3]) and n_moves (int32 [1]): what page_copy is to do; missing (int32 [1]): free pages that lack (then
-    nothing has changed)."""
+    nothing has changed).  Of a shared page that is replaced the rows in front of start[b] are copied, none from tokens[b] on."""
     n, device = tables.requests, tables._device
     if moves.shape[0] < n:
         raise ValueError(f"moves: expected at least {n} rows")
