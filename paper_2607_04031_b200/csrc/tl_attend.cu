@@ -119,8 +119,12 @@ static auto attend_tc_of(int format) {
 //                                    16 over 2000 (10.9) 116 / 94, 92 / 91; 192 rows, 8 over 8000 (21.6) 124 / 103, 120 / 108
 //                                    160 rows, 8 over 8000 E4M3 97 / 108
 // Blocks of 256 fetch and convert every tile for two streams at once, but need rows to fill them and more than a few
-// tiles per SM to pay for the wider joins.  The lengths are on the device; what the host knows is that they fit the table's rows and,
-// pages being one request's alone, the pool: a table as wide as the longest sequence there may ever be says little.
+// tiles per SM to pay for the wider joins.  The lengths are on the device; the host takes the table's rows for them, or the pool where
+// that is less, each of its pages counted once: a table as wide as the longest sequence there may ever be says little (room for 262144,
+// a pool that just suffices, 8 requests over 500 by the pool / by the table: bf16 36 / 60, E4M3 28 / 54, 4 bits 30 / 56).  It is an estimate:
+// requests that share pages (tl_page_fork) may be longer together than the pool, and then get blocks of 128 where 256 would do.
+// 256 rows each behind one shared prompt, 128 / 256: 8 over 4100 bf16 85 / 89, E4M3 93 / 93, 4 bits 112 / 116; 16 over 4100 136 / 136,
+// 155 / 146, 185 / 181; 64 over 2000 271 / 232, 292 / 251, 357 / 314.
 constexpr int kBlockRowsFrom = 192, kBlockTilesFrom = 8;
 static int attend_plan(const tl_kv_cache* cache, const tl_kv_batch* batch, int q_heads, AttendPlan* plan) {
     const int group = q_heads / cache->heads;
