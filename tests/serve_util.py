@@ -75,6 +75,34 @@ class Pool4(kv_util.Pool):
                 *(move(t).view(torch.float8_e4m3fn) for t in (self.kg, self.vg)))
 
 
+def weights_and_scales(q, keys, scales, ctx, sees, scale):
+    """One request in fp64: softmax weights [q_heads, n, positions] and the largest weight times its value's scale [n, q_heads]; q
+    [n, q_heads, dim], keys [positions, heads, dim], scales (of the values) [positions, heads]."""
+    n, hq, dim = q.shape
+    heads = keys.shape[1]
+    z = torch.einsum("jhd,thgd->hgtj", keys, q.double().view(n, heads, hq // heads, dim)) * scale
+    seen = torch.ones(n, keys.shape[0], dtype=torch.bool)
+    seen[:, ctx:] = sees
+    z = z.masked_fill(~seen, -math.inf)
+    p = torch.nan_to_num(torch.softmax(z, -1))                           # heads, group, n, positions
+    largest = (p * scales.T[:, None, None]).amax(-1)                     # heads, group, n
+    return p.flatten(0, 1), largest.permute(2, 0, 1).reshape(n, hq)
+
+
+def attention_bound4(out, mass, big, largest, values, scales, dim, scale):
+    """How far a bf16 result over a 4-bit cache may be from fp64.
+
+    The result's rounding, 2^-8 of it.  A weight times its value's scale enters the second product in f16: 2^-11 of it, and steps of
+    2^-31 of the row's largest such product (`largest`, weights as shares of their sum): the sum over the positions of that times
+    |code * group scale|.  Scores as in kv_util.attention_bound, twice.  The second product sums one product per position in fp32 with
+    truncation: 2^-23 each of at most sum p |v|."""
+    length, heads = values.shape[:2]
+    score = dim * 2.0 ** -23 * big * abs(scale) + 2.0 ** -20
+    codes = (values.abs() / torch.where(scales > 0, scales, torch.ones_like(scales))[..., None]).sum(0)         # heads, dim
+    flush = 2.0 ** -31 * largest[..., None] * codes.repeat_interleave(out.shape[1] // heads, 0)
+    return 2.0 ** -8 * out.abs() + (2.0 ** -11 + 2 * score + length * 2.0 ** -23)[..., None] * mass + flush + 1e-30
+
+
 def cos_sin(turns, positions, amplitude=1.0):
     """fp64 [tokens, pairs] from the fixed-point frequencies: the angle is exact."""
     c, s = [], []
