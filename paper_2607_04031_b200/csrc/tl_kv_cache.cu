@@ -110,14 +110,15 @@ __device__ __forceinline__ int warp_request_of(const KvBatchView& bv, int row) {
 }
 
 // Address of a position's row in the cache (keys or values), or null when there is no page for it.  extra: 0 the row's scale in
-// *scale, n > 0 word n - 1 of its group scales in its place.
+// *scale, n > 0 (kFour) word n - 1 of its group scales in its place.
+template <bool kFour>
 __device__ __forceinline__ char* kv_row(const KvView& c, const KvBatchView& bv, int b, int pos, int which, int head,
                                         float** scale, int group_words, int extra) {
     if (pos < 0 || pos >= kv_room(bv, c.page_shift)) return nullptr;
     const int64_t page = bv.page_table[int64_t(b) * bv.table_stride + (pos >> c.page_shift)];
     if (page < 0 || page >= c.pages) return nullptr;
     const int line = pos & ((1 << c.page_shift) - 1);
-    if (scale && extra <= 0) *scale = c.scale[which] + page * c.scale_page_stride + int64_t(head) * c.scale_head_stride + line;
+    if (scale && (!kFour || extra <= 0)) *scale = c.scale[which] + page * c.scale_page_stride + int64_t(head) * c.scale_head_stride + line;
     else if (scale) *scale = reinterpret_cast<float*>(c.group[which] + page * c.group_page_stride + int64_t(head) * c.group_head_stride) + line * group_words + extra - 1;
     return c.base[which] + page * c.page_stride + int64_t(head) * c.head_stride + line * c.token_stride;
 }
@@ -381,10 +382,11 @@ constexpr int kCommitAhead = 4;
 
 // One CTA per request, so that the new length (which may overwrite batch.start) is written when every thread has read
 // the old one.
+template <bool kFour>
 __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommitParams p) {
     pdl_wait();
     pdl_launch_dependents();
-    const int lanes = p.chunks + 1 + p.group_words;           // the extra ones move the scales
+    const int lanes = p.chunks + 1 + (kFour ? p.group_words : 0);           // the extra ones move the scales
     const int b = blockIdx.x;
     const KvRequest r = kv_request(p.batch, p.cache.page_shift, b);
     const int n = int(min(int64_t(min(max(p.n_accepted[b], 0), r.n)), p.accepted_stride));
@@ -408,7 +410,7 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommi
                 }
                 if (a == i) continue;                         // it is there already
                 float* s = nullptr;
-                const char* src = kv_row(p.cache, p.batch, b, r.start + a, which, head, has_scales ? &s : nullptr, p.group_words, l - p.chunks);
+                const char* src = kv_row<kFour>(p.cache, p.batch, b, r.start + a, which, head, has_scales ? &s : nullptr, p.group_words, l - p.chunks);
                 if (!src) {
                     atomicCAS(p.status, 0u, kBadPage);
                     continue;
@@ -421,7 +423,7 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommi
             for (int k = 0; k < kCommitAhead; ++k) {
                 if (!have[k]) continue;
                 float* s = nullptr;
-                char* dst = kv_row(p.cache, p.batch, b, r.start + i0 + k, which, head, has_scales ? &s : nullptr, p.group_words, l - p.chunks);
+                char* dst = kv_row<kFour>(p.cache, p.batch, b, r.start + i0 + k, which, head, has_scales ? &s : nullptr, p.group_words, l - p.chunks);
                 if (!dst) continue;                           // a page in front of one that exists: reported by the writer
                 if (l < p.chunks) *reinterpret_cast<uint4*>(dst + l * 16) = row[k];
                 else *s = scale[k];
@@ -549,7 +551,7 @@ int tl_kv_commit(const tl_kv_cache* cache, const tl_kv_batch* batch, const int32
     p.group_words = cache->format == TL_KV_E2M1 ? cache->head_dim / 64 : 0;
     const int64_t items = int64_t(2) * cache->heads * (p.chunks + 1 + p.group_words);
     const int threads = int(std::min<int64_t>(ceil_div(items, 32) * 32, kCommitThreads));
-    return kv_launch(kv_commit_kernel, dim3(unsigned(p.batch.requests)), threads, static_cast<cudaStream_t>(cuda_stream), p);
+    return kv_launch(p.group_words ? kv_commit_kernel<true> : kv_commit_kernel<false>, dim3(unsigned(p.batch.requests)), threads, static_cast<cudaStream_t>(cuda_stream), p);
 }
 
 int tl_tree_mask(const int32_t* d_parents, const int32_t* d_token_offsets, int requests, int tokens, uint32_t* d_mask,
