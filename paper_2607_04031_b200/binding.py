@@ -465,6 +465,10 @@ _KV_FORMATS = {torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_E4M3, torch.int8
 _ELEMS = {torch.bfloat16: ELEM_BF16, torch.float32: ELEM_F32}
 
 
+# (_ref of the descriptions below is their address: a ctypes reference would refer back to the object that holds it, and device memory
+# would wait for Python's cycle collector.)
+
+
 class KvCache(ctypes.Structure):
     """tl_kv_cache; keeps the tensors it was made from alive."""
     _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("pages", _i64), ("page_stride", _i64),
@@ -541,7 +545,7 @@ def kv_cache(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = No
         c.group_page_stride, c.group_head_stride = k_group.stride()[:2]
     elif k_group is not None or v_group is not None:
         raise ValueError("only a 4-bit cache has group scales")
-    c._tensors, c._ref, c._device = (k, v, k_scale, v_scale, k_group, v_group), ctypes.byref(c), k.get_device()
+    c._tensors, c._ref, c._device = (k, v, k_scale, v_scale, k_group, v_group), ctypes.addressof(c), k.get_device()
     for t, name in ((v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale"), (k_group, "k_group"), (v_group, "v_group")):
         if t is not None and t.get_device() != c._device:
             raise _elsewhere(t, name, c._device)
@@ -559,7 +563,7 @@ def kv_batch(page_table: torch.Tensor, start: torch.Tensor, token_offsets: torch
     b.token_offsets = _int32(token_offsets, "token_offsets", (n + 1,), device)
     b.table_stride = page_table.shape[1]
     b.requests, b.tokens = n, int(tokens)
-    b._tensors, b._ref = (page_table, start, token_offsets), ctypes.byref(b)
+    b._tensors, b._ref = (page_table, start, token_offsets), ctypes.addressof(b)
     return b
 
 
@@ -748,7 +752,7 @@ def rope(turns: torch.Tensor, layout: int = ROPE_HALF, amplitude: float = 1.0) -
         raise ValueError("turns: expected a contiguous tensor")
     r = Rope()
     r.turns, r.amplitude, r.rotary_dim, r.layout = turns.data_ptr(), amplitude, 2 * turns.shape[0], layout
-    r._tensors, r._ref, r._device = (turns,), ctypes.byref(r), turns.get_device()
+    r._tensors, r._ref, r._device = (turns,), ctypes.addressof(r), turns.get_device()
     return r
 
 
@@ -833,7 +837,7 @@ def page_tables(page_table: torch.Tensor, held: torch.Tensor, holders: torch.Ten
     t.page_table = _int32(page_table, "page_table", page_table.shape, device)
     t.held = _int32(held, "held", (t.requests,), device)
     t.holders = _int32(holders, "holders", holders.shape, device)
-    t._tensors, t._ref = (page_table, held, holders), ctypes.byref(t)
+    t._tensors, t._ref = (page_table, held, holders), ctypes.addressof(t)
     return t
 
 
