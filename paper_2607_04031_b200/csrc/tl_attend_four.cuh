@@ -19,13 +19,16 @@
 // masked positions may hold: as over an 8-bit cache; no code or group scale reads as infinite or NaN, so positions past the end need
 // no zeros in their place.
 //
-// Measured choices.  Queries in registers took as long with one block of 8 rows and 2 to 12 % longer with two and four.  Two sub-tiles a
-// turn: 32 requests of one token over 4100 (cold) 48 us, one a turn 54; beyond 32 accumulators one a turn took up to 13 % less with few
-// requests and 3 % more to 1 % less with 64.  CTAs per SM, the same call: four 46 to 48 us, three 50, five (too few registers) 56 to 58; with 64
-// accumulators three in place of two took 8 to 12 % less at 4 requests over 4100 and up to 7 % more elsewhere.
+// Measured choices.  Queries in registers took as long with one block of 8 rows and 2 to 12 % longer with two and four.  CTAs per SM and
+// sub-tiles a turn with the queries where they are (64 query and 8 key/value heads of 128, contexts of half the length to all of it, us as
+// it is / one sub-tile a turn / three CTAs / five CTAs): 1 request of one token over 4100 14.9 / 14.4 / 14.4 / 16.7, 4 over 4100 17.0 / 16.2 /
+// 17.5 / 20.5, 32 over 4100 40.8 / 40.4 / 40.1 / 49.5, 64 over 2000 43.2 / 41.6 / 44.6 / 49.3; 1 over 407 (32 / 4 heads) 9.8 / 9.3 / 9.8 / 10.2.
+// (While queries lay in registers two sub-tiles took 48 us for 32 over 4100 where one took 54; now they make no odds, or 1 to 5 % the wrong
+// way.)  With 64 accumulators two CTAs / three: 32 requests of one token over 4100, heads of 256, 65.3 / 60.7; two tokens each, 64 over 2000
+// 57.6 / 54.8, 16 over 4100 32.9 / 33.2; heads of 64, four tokens each, 4 over 4100 20.8 / 21.7, 16 32.8 / 34.7, 64 over 2000 57.5 / 56.9.
 //
 // What bounds it: 32 requests of one token over 4100 (64 query and 8 key/value heads of 128, 122 MB): 41 us, floor 18.6.  8.6 us pass
-// outside of the loop (launch, ranges, queries, joins); 20 million warp instructions keep the ALUs, which run unpacking and softmax at half
+// outside of the loop (launch, ranges, queries, joins; as 29 below from copies of an earlier form); 20 million warp instructions keep the ALUs, which run unpacking and softmax at half
 // rate, busy for 48 % and the issue slots for 58 % of the time with four warps per scheduler; the copies alone (no arithmetic)
 // take 29.  Bulk copies in place of cp.async: as fast issued by each warp, 62 us by a warp of their own.
 #pragma once

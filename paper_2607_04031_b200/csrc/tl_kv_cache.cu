@@ -196,8 +196,8 @@ __global__ void __launch_bounds__(kCopyThreads) kv_read_kernel(const KvCopyParam
 // The same two for 4-bit caches.  A lane owns the 16 elements of a group scale (32 bytes of bf16, 8 of codes), a group of kDim / 16
 // lanes a row's head, and a warp several neighbouring rows, whose places are looked up together: with 4 bits a row of 8 heads is
 // 512 bytes, too little for a warp to wait for alone.  8192 rows of 8 heads x 128 appended and 26200 read back, from and to bf16: 42 us
-// for 187 MB (floor 28.5); one row per warp and eight elements per lane 55 us.  Apart and cold: append 16.6 us for 44 MB, bound by the
-// quotients' instructions (issue slots 69 %), read 29 us for 139 MB, most of them written (issue slots 59 %).
+// for 187 MB (floor 28.5); one row per warp and eight elements per lane 55 us.  Apart and cold: append 16.6 to 17.8 us for 44 MB, bound by the
+// quotients' instructions (issue slots 65 to 69 %), read 29 us for 139 MB, most of them written (issue slots 59 %).
 // Heads per warp, append and read together, caches cold: 8 read and 4 appended at a time 50 us, 4 and 4 48, 4 and 2 46, 2 and 2 50.
 constexpr int kFourHeads = 4, kFourAppendHeads = 2, kFourReadCtas = 4;
 

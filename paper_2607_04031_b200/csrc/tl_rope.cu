@@ -120,6 +120,9 @@ __global__ void __launch_bounds__(kRopeThreads, kF32 ? 3 : 4) rope_rows_kernel(c
 }
 
 // Any even sizes, by elements: a thread owns a pair, or an element that stays, of one token and takes heads in turn.
+// 8192 tokens x 72 heads of 128, bf16, 36 dimensions turned 210 us, 100 turned 194 (either layout; floor 46), fp32 with 36 280 (floor 92);
+// 72 heads of 90 91 (32); 32 tokens of 72 heads 2.9.  Accesses of 2 and 4 bytes bound it: 2.5 times the vectors' warp instructions, 211 MB
+// read and 136 written in 206 us, issue slots 27 % with 73 % of the warps.
 template <bool kF32>
 __global__ void __launch_bounds__(kRopeThreads) rope_rows_any_kernel(const RopeRowsParams p) {
     pdl_wait();
@@ -226,8 +229,10 @@ __device__ __forceinline__ void rope_partners(const RopeView& r, const char* row
 }
 
 // A warp takes one row's heads, kCopyAhead groups of them: of the queries, of the keys or of the values (blockIdx.y).
-// A step of 32 tokens (64 query and 8 key/value heads of 128): 8 us, a chain of loads (the row's request, its page, positions, angles);
-// rows and partners are asked for ahead of it.
+// A step of 32 tokens (64 query and 8 key/value heads of 128): 8 us with the host's call, 4.4 back to back over bf16 and 6.1 over 4 bits, a
+// chain of loads (the row's request, its page, positions, angles); rows and partners are asked for ahead of it.  It is made for steps: 1024
+// rows take 19 to 21 us, 8192 119 (bf16), 132 (8 bits) and 135 (4 bits), where turning and appending by calls of their own take 66 to 70: a
+// warp works out its angles for every eight heads of a row, partners are read twice, 80 to 90 million warp instructions, issue slots 59 %.
 template <int kFmt, int kDim, bool kF32>
 __global__ void __launch_bounds__(kCopyThreads, 2) rope_append_kernel(const RopeAppendParams p) {
     pdl_wait();
